@@ -76,12 +76,18 @@ typedef enum ms_op_kind {
     MS_OP_CONV2D_TRANSPOSED_NHWC = 7, /* Y = act(bias + convT(X, W)): the adjoint of CONV2D_NHWC in X; X NHWC,
                                         W [KH][KW][Cin][Cout]                (T2D) */
     MS_OP_CONV1D_NWC = 8,    /* Y = act(bias + conv(X, W)), X [N][L][Cin], W [K][Cin][Cout]  (C1D) */
-    MS_OP_CONV3D_NDHWC = 9   /* Y = act(bias + conv(X, W)), X [N][D][H][W][Cin], W [K][K][K][Cin][Cout]  (C3D) */
+    MS_OP_CONV3D_NDHWC = 9,  /* Y = act(bias + conv(X, W)), X [N][D][H][W][Cin], W [K][K][K][Cin][Cout]  (C3D) */
+    /* layers of language models: one kernel for all sizes, see below */
+    MS_OP_RMS_NORM = 10,     /* H = X + R, Y = quantise(H / sqrt(mean(H^2) + eps) * W) */
+    MS_OP_SCALED_GEMM = 11,  /* C[i][j] = sum_b SA[i][b] SB[j/128][b] sum_{k in block b of 128} A[i][k] B[j][k] */
+    MS_OP_GROUPED_GEMM = 12, /* C[t][j] = sum_k A[t][k] B[e(t)][k][j], rows t sorted by expert e */
+    MS_OP_GROUPED_WGRAD = 13 /* D[e][i][j] = sum_{t of expert e} P[t][i] Q[t][j]: the gradient of B above */
 } ms_op_kind;
 
 typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 = 4,
                         MS_F8E4M3 = 5 /* input only, GEMM / BMM on the matrix cores: 8-bit float, 4 exponent bits (bias 7),
-                                         3 mantissa bits, no infinities, 0x7f / 0xff NaN; fp32 accumulate, output F16 or F32 */
+                                         3 mantissa bits, no infinities, 0x7f / 0xff NaN; fp32 accumulate, output F16 or F32.
+                                         Of SCALED_GEMM and GROUPED_GEMM the inputs, of RMS_NORM the output, with scales */
 } ms_dtype;
 
 /*
@@ -109,7 +115,33 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  * dense default of the op kind): A element (b,i,k) at b*a[0] + i*a[1] + k*a[2];
  * B element (b,k,j) at b*b[0] + k*b[1] + j*b[2].
  * Inputs of a launch: GEMM/BMM {A, B}; CONV {X, W, bias or NULL}; DW {X, W}; SOFTMAX/NORM {X}.
+ *
+ * Layers of language models.  Sizes are arguments of their kernels, not constants: operators that differ in sizes only share
+ * compiled kernels, and creating one for every batch costs no compilation.  stride, pad, relu and dilation are 0.
+ *   RMS_NORM      dims M, N, eps in units of MS_EPS_UNIT; F32, F16 or BF16 in.  Inputs {X [M][N], W [N], R [M][N] or NULL}, outputs
+ *                 {Y [M][N], S, H}.  has_bias 1: a residual R is added, H [M][N] = X + R rounded once to in_dtype, and the norm is that of
+ *                 the rounded H, so that it can be computed again from what is kept; H may be X or R itself.  has_bias 0: R and H are
+ *                 not read, H = X.  y = h / sqrt(sum(h^2) / N + eps) * w in fp32.  out_dtype = in_dtype: Y = y rounded once, S is not
+ *                 read.  out_dtype F8E4M3: with S[i][b] = max(max_{128 columns of block b} |y|, 448 * 2^-126) / 448 (fp32, [M][ceil(N / 128)]) Y is y / S rounded
+ *                 (to the nearest 8-bit float, ties to even); a NaN in a block makes S and the block NaN.  a_strides[1] = elements between rows of X (0 = N);
+ *                 b_strides 0.  Tensors need only be aligned to their elements.
+ *   SCALED_GEMM   dims M, N, K; in F8E4M3, out F16, BF16 or F32.  Inputs {A [M][K], B [N][K], SA fp32 [M][ceil(K / 128)],
+ *                 SB fp32 [ceil(N / 128)][ceil(K / 128)]}.  The products of a block of 128 k values are summed by the matrix cores,
+ *                 the blocks in fp32.
+ *   GROUPED_GEMM  dims E, T, N, K (E <= MS_MAX_EXPERTS); F16 or BF16 in, the same or F32 out, or F8E4M3 as above.  Inputs {A [T][K], B [E][N][K],
+ *                 offsets int32 [E + 1] (device memory), SA [T][ceil(K / 128)], SB [E][ceil(N / 128)][ceil(K / 128)]} (the scales for F8E4M3 only).  Expert e has
+ *                 the rows from offsets[e] up to offsets[e + 1] (none if that is not larger) of A and C; rows of no expert are left as they were in C.
+ *                 offsets do not decrease; values outside [0, T] count as the nearer end.  b_strides {N * K, 1, K} (the default) or, 2-byte inputs,
+ *                 {K * N, N, 1}: B stored [E][K][N], as the gradient of A needs it.
+ *   GROUPED_WGRAD dims E, T, I, J; F16 or BF16 in, the same or F32 out.  Inputs {P [T][I], Q [T][J], offsets}, output D [E][I][J], written
+ *                 whole: zeros for an expert without rows.
+ *   Strides of the products may exceed the dense ones (rows of at most MS_MAX_ROW_BYTES); A, P and Q are shared by the experts, their stride [0] is not read.  Tensors of
+ *   the products are aligned to 16 bytes (scales and offsets to 4), and several instances need copies of whole 16 bytes.
+ *   Loads of 16 bytes need rows and K (P and Q: I and J) of whole 16 bytes; other sizes run a slower kernel.
  */
+#define MS_EPS_UNIT 1e-12
+#define MS_MAX_EXPERTS 1024
+#define MS_MAX_ROW_BYTES (4 << 20)
 typedef struct ms_op_desc {
     int32_t kind;
     int32_t in_dtype;
@@ -148,7 +180,7 @@ int32_t ms_op_loops(const ms_op *op, ms_loop *loops /* [MS_MAX_LOOPS] */, int32_
  * bytes = every input and output tensor moved once. */
 int32_t ms_op_work(const ms_op *op, double *flop, double *bytes);
 /* Byte size of input `idx` / of the output, for one instance. */
-int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx /* -1 = output */, int64_t *bytes);
+int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx /* -1 = output; RMS_NORM: -2 = S, -3 = H */, int64_t *bytes);
 
 /* ------------------------------------------------------------------ S(e0) */
 
@@ -221,6 +253,9 @@ typedef enum ms_slot_id {
                                  does not depend on how the workgroups are scheduled.  S must divide k0; persistent
                                  workgroups (reorder 3, compute_at 2..4) and cache_write 1 own the whole reduction
                                  and the epilogue and need S = 1 */
+    ,
+    MS_SLOT_BLOCK = 14        /* categorical (layers of language models): what a workgroup works on.  0 = as the rules say, by the
+                                 operator's sizes.  Products: 1000 * rows + columns of its tile.  RMS_NORM: wavefronts that share a row */
 } ms_slot_id;
 
 /* Tensorize candidates: (m, n, k) of one matrix-core instruction.  The code
@@ -288,7 +323,8 @@ typedef struct ms_slot {
                                          all-ones default of earlier tuning records) mean the same */
 
 typedef enum ms_family { MS_FAM_GEMM_ALU = 0, MS_FAM_GEMM_MFMA = 1, MS_FAM_DWCONV = 2,
-                         MS_FAM_REDUCE = 3 /* softmax, norm: rows reduced by groups of lanes */ } ms_family;
+                         MS_FAM_REDUCE = 3, /* softmax, norm: rows reduced by groups of lanes */
+                         MS_FAM_RMS_NORM = 4, MS_FAM_RAGGED = 5 /* SCALED_GEMM, GROUPED_GEMM, GROUPED_WGRAD */ } ms_family;
 
 typedef struct ms_space {
     int32_t family;
@@ -388,6 +424,9 @@ int32_t ms_trace_mutate(const ms_space *space, const ms_trace *in, uint64_t seed
 int32_t ms_trace_to_text(const ms_op *op, const ms_space *space, const ms_trace *trace,
                          char *buf, size_t cap, size_t *needed);
 int32_t ms_trace_from_text(const ms_space *space, const char *text, ms_trace *out);
+/* The trace that leaves every decision to the library's rules (candidate 0 of MS_SLOT_BLOCK), for callers that neither search nor
+ * sample.  UNSUPPORTED if the space has a decision that no rule makes. */
+int32_t ms_trace_default(const ms_space *space, ms_trace *out);
 
 /* ------------------------------------------------------------------ g(e0,tau) */
 
@@ -417,9 +456,14 @@ typedef enum ms_body {
                                 of 32 channels in LDS, read under every tap; body_tile packs the tile */
     MS_BODY_CONV_PLANES = 8, /* the same of MS_BODY_IMAGE_ROWS: persistent workgroups, a filter plane's rows and weights loaded straight
                                 into LDS; body_tile = 32-pixel tiles of a wavefront */
+    MS_BODY_RMS_ROWS = 10,   /* RMS_NORM: rows in the registers of a workgroup; body_tile = wavefronts that share a row */
+    MS_BODY_RAGGED_TILES = 11, /* products over rows by expert: tiles whose operands lie in LDS; body_tile = 1000 * rows + columns */
+    MS_BODY_RAGGED_ROWS = 12,  /* the same of few rows for each expert: wavefronts of a workgroup share its reduction */
     MS_BODY_FEW_ROWS = 9     /* the same of a nest over up to 128 rows times a row-major matrix (fp16, bf16), of launches of up to 64 x 64
                                 outputs per compute unit: wavefronts of a workgroup share its reduction; body_tile packs the tile */
 } ms_body;
+
+/* Bodies 10 to 12 are those of the layers of language models, whose kernels take sizes as arguments. */
 
 /* What the trace interpreter derives.  Unused fields are zero.  With bodies 1 to 3 and 6, block_*, grid, threads,
  * waves, acc_per_thread, lds_bytes, vec and vec_b are those of the kernel that runs, and so are the splits ti, tj, tc and tk
@@ -529,7 +573,7 @@ int32_t ms_jit_stats(int64_t *compiled, int64_t *from_disk, int64_t *from_memory
 
 /* Enqueue one execution over `instances` instances on `stream`.  inputs /
  * outputs: host arrays of device pointers (see ms_op_desc for the order; one
- * output).  16-byte aligned pointers are always enough; the kernels of MS_BODY_ROW_VECTORS, MS_BODY_STRIPS and
+ * output, RMS_NORM three, NULL where it has none).  16-byte aligned pointers are always enough; the kernels of MS_BODY_ROW_VECTORS, MS_BODY_STRIPS and
  * MS_BODY_IMAGE_ROWS need tensors aligned to their elements only (the bias to 16 bytes).  workspace: device pointer, 16-byte aligned, of at least instances x
  * workspace_bytes (ms_variant_info), owned by the caller and not shared with a
  * launch that may run at the same time; NULL if that is 0.  Its contents need no
@@ -589,6 +633,9 @@ typedef struct ms_bufset {
 } ms_bufset;
 
 /*
+ * Operators of several outputs: `output` is one block that holds them one after the other, and an operator of five inputs has
+ * its fourth and fifth in one block at inputs[3]; every tensor (all instances of it) starts at a multiple of 256 bytes from the block.
+ *
  * One repeat = hipEventRecord, launches_per_repeat launches back to back on
  * `stream` (launch l uses buffer set l mod n_sets), hipEventRecord, wait.
  * Per-launch time = elapsed / launches_per_repeat.  `warmup` untimed launches

@@ -13,11 +13,11 @@ LIB_PATH = os.path.join(HERE, "libms.so")
 
 MS_OK, MS_ERR_BAD_ARG, MS_ERR_INVALID_TRACE, MS_ERR_UNSUPPORTED, MS_ERR_COMPILE, MS_ERR_HIP, MS_ERR_NOMEM = range(7)
 (OP_GEMM, OP_BMM_NT, OP_BMM_NN, OP_CONV2D_NHWC, OP_DWCONV2D_NHWC, OP_SOFTMAX, OP_NORM,
- OP_CONV2D_TRANSPOSED_NHWC, OP_CONV1D_NWC, OP_CONV3D_NDHWC) = range(10)
+ OP_CONV2D_TRANSPOSED_NHWC, OP_CONV1D_NWC, OP_CONV3D_NDHWC, OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD) = range(14)
 F32, F16, BF16, I8, I32 = range(5)
 SLOT_PERFECT_TILE, SLOT_CATEGORICAL = 0, 1
 (SLOT_TENSORIZE, SLOT_TILE_I, SLOT_TILE_J, SLOT_TILE_C, SLOT_TILE_K, SLOT_UNROLL, SLOT_CACHE_READ, SLOT_VECTORIZE,
- SLOT_STORAGE_ALIGN, SLOT_REORDER, SLOT_VECTORIZE_B, SLOT_CACHE_WRITE, SLOT_COMPUTE_AT, SLOT_RFACTOR) = range(14)
+ SLOT_STORAGE_ALIGN, SLOT_REORDER, SLOT_VECTORIZE_B, SLOT_CACHE_WRITE, SLOT_COMPUTE_AT, SLOT_RFACTOR, SLOT_BLOCK) = range(15)
 SPACE_TENSORIZE, SPACE_CACHE_READ, SPACE_VECTORIZE, SPACE_UNROLL, SPACE_STORAGE_ALIGN, SPACE_REORDER, SPACE_CACHE_WRITE = 1, 2, 4, 8, 16, 32, 64
 SPACE_COMPUTE_AT = 128
 SPACE_TENSORIZE_F32 = 0x100  # opt-in: fp32 operators on the fp32 matrix-core intrinsics
@@ -25,9 +25,10 @@ SPACE_TAP_ROWS = 0x200  # opt-in: conv2d reduction laid out as filter rows (firs
 SPACE_RFACTOR = 0x400  # opt-in: sample the split of the reduction across workgroups (needs a workspace)
 SPACE_DEFAULT = 0xFF
 STATIC_WORKSPACE_BYTES = 32 << 20
-FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE = range(4)
+FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE, FAM_RMS_NORM, FAM_RAGGED = range(6)
 (BODY_NEST, BODY_ROW_VECTORS, BODY_STRIPS, BODY_IMAGE_ROWS, BODY_PHASES, BODY_DOUBLE_STEPS, BODY_CONV_STEPS, BODY_CONV_PATCH, BODY_CONV_PLANES,
- BODY_FEW_ROWS) = range(10)
+ BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS) = range(13)
+EPS_UNIT, MAX_EXPERTS, SCALE_BLOCK = 1e-12, 1024, 128
 MAX_SLOTS, MAX_FACTORS, MAX_CANDS, MAX_LOOPS = 16, 4, 12, 8
 
 F8E4M3 = 5
@@ -174,6 +175,7 @@ SYMBOLS = {
     "ms_trace_sample_valid": (C.c_int32, [C.c_void_p, _P(ms_space), C.c_uint64, C.c_uint64, C.c_int32, _P(ms_trace)]),
     "ms_trace_mutate": (C.c_int32, [_P(ms_space), _P(ms_trace), C.c_uint64, _P(ms_trace)]),
     "ms_trace_to_text": (C.c_int32, [C.c_void_p, _P(ms_space), _P(ms_trace), C.c_char_p, C.c_size_t, _P(C.c_size_t)]),
+    "ms_trace_default": (C.c_int32, [_P(ms_space), _P(ms_trace)]),
     "ms_trace_from_text": (C.c_int32, [_P(ms_space), C.c_char_p, _P(ms_trace)]),
     "ms_trace_validate": (C.c_int32, [C.c_void_p, _P(ms_space), _P(ms_trace), _P(ms_variant_params)]),
     "ms_get_limits": (C.c_int32, [_P(ms_limits)]),
@@ -350,6 +352,33 @@ def norm_op(B, M, N, in_dtype="f32"):
     return Op(OP_NORM, in_dtype, "f32", [B, M, N])
 
 
+# ---- layers of language models (ms_op_desc has their definitions)
+def rms_norm_op(M, N, in_dtype="bf16", out_dtype=None, residual=True, eps=1e-6, **kw):
+    """RMS norm of rows; inputs (X [M, N], W [N], R [M, N] with a residual), outputs (Y [M, N], S, H): S fp32 [M, ceil(N / 128)] for
+    out_dtype "f8", H = X + R [M, N] with a residual, None where there is none."""
+    if not 0 <= eps <= 1:
+        raise ValueError("eps = %r" % (eps,))
+    return Op(OP_RMS_NORM, in_dtype, out_dtype or in_dtype, [M, N, round(eps / EPS_UNIT)], has_bias=residual, **kw)
+
+
+def scaled_gemm_op(M, N, K, out_dtype="bf16", **kw):
+    """C [M, N] of 8-bit floats A [M, K] and B [N, K] with scales SA [M, ceil(K / 128)], SB [ceil(N / 128), ceil(K / 128)]; inputs (A, B, SA, SB)."""
+    return Op(OP_SCALED_GEMM, "f8", out_dtype, [M, N, K], **kw)
+
+
+def grouped_gemm_op(E, T, N, K, rows_of_k=True, in_dtype="bf16", out_dtype=None, **kw):
+    """C [T, N]: rows of A [T, K], sorted by expert, times their expert's matrix of B [E, N, K] (rows_of_k) or [E, K, N]; inputs
+    (A, B, offsets int32 [E + 1]), for "f8" also (SA, SB)."""
+    if not rows_of_k and "b_strides" not in kw:
+        kw["b_strides"] = [K * N, N, 1]
+    return Op(OP_GROUPED_GEMM, in_dtype, out_dtype or ("bf16" if in_dtype == "f8" else in_dtype), [E, T, N, K], **kw)
+
+
+def grouped_wgrad_op(E, T, I, J, in_dtype="bf16", out_dtype=None, **kw):
+    """D [E, I, J]: of each expert the sum of P[t, i] Q[t, j] over its rows t of P [T, I], Q [T, J]; inputs (P, Q, offsets int32 [E + 1])."""
+    return Op(OP_GROUPED_WGRAD, in_dtype, out_dtype or in_dtype, [E, T, I, J], **kw)
+
+
 MAX_MODULES = 16
 
 
@@ -404,6 +433,13 @@ def trace_sample(space, seed, index):
 def trace_sample_valid(op, space, seed, index, max_tries=1000):
     t = ms_trace()
     _check(lib().ms_trace_sample_valid(op.handle, C.byref(space), seed, index, max_tries, C.byref(t)))
+    return t
+
+
+def default_trace(space):
+    """The trace that leaves every decision to the library's rules (layers of language models)."""
+    t = ms_trace()
+    _check(lib().ms_trace_default(C.byref(space), C.byref(t)))
     return t
 
 
@@ -576,7 +612,7 @@ class Variant:
         return ws.value
 
     def launch(self, inputs, output, instances=1, stream=None, workspace=None):
-        """inputs / output / workspace: device pointers (ints)."""
+        """inputs / output / workspace: device pointers (ints); output: a sequence of them for an operator of several outputs."""
         rc = _launch_native(self._address, inputs, output, instances, stream, workspace)
         if rc:
             _check(rc)
@@ -587,8 +623,8 @@ class Variant:
 
     def launch_static(self, inputs, output, instances=1, stream=None):
         """launch() with the workspace taken from the library's built-in array; allocates nothing."""
-        ins = (C.c_void_p * 4)(*[C.c_void_p(p) for p in inputs])
-        outs = (C.c_void_p * 1)(C.c_void_p(output))
+        ins = (C.c_void_p * 8)(*[C.c_void_p(p) for p in inputs])
+        outs = (C.c_void_p * 8)(*[C.c_void_p(p) for p in (output if isinstance(output, (list, tuple)) else (output,))])
         _check(lib().ms_variant_launch_static(self.handle, ins, outs, instances, stream))
 
     def measure(self, bufsets, warmup=2, repeats=5, launches_per_repeat=20, instances=1, stream=None):

@@ -1,0 +1,128 @@
+// Shared by the kernels of products over rows that lie sorted by expert.
+
+// As RaggedArgs in ms_internal.h: distances in bytes.  depth, cols and rows of a gradient of weights are T, J and I.
+struct ragged_args {
+    const char *a, *b;
+    const int *offsets;
+    const float *sa, *sb;
+    char *c;
+    long a_row, b_row, b_expert;
+    long a_inst, b_inst, sa_inst, sb_inst, c_inst;
+    int rows, cols, depth, experts;
+};
+
+typedef unsigned u4_t __attribute__((ext_vector_type(4)));
+typedef float f4_t __attribute__((ext_vector_type(4)));
+typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
+typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
+typedef int i8v_t __attribute__((ext_vector_type(8)));
+
+// One matrix-core step.  The operands are swapped, so that a lane holds four consecutive columns of one row: rows lane % 16, columns
+// 4 * (lane / 16) and on.
+#if IN_DT == DT_F8E4M3
+struct frag_t { u4_t v[2]; }; // 32 k values
+__device__ __forceinline__ f4_t mfma(const frag_t &b, const frag_t &a, f4_t c)
+{
+    // format selectors 0 = this 8-bit float for both operands; zero scale operands select the unscaled form
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i8v_t, b), __builtin_bit_cast(i8v_t, a), c, 0, 0, 0, 0, 0, 0);
+}
+#else
+struct frag_t { u4_t v[1]; }; // 8 k values
+__device__ __forceinline__ f4_t mfma(const frag_t &b, const frag_t &a, f4_t c)
+{
+#if IN_DT == DT_F16
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, b.v[0]), __builtin_bit_cast(h8_t, a.v[0]), c, 0, 0, 0);
+#else
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, b.v[0]), __builtin_bit_cast(b8_t, a.v[0]), c, 0, 0, 0);
+#endif
+}
+#endif
+constexpr int ES = sizeof(in_t), KQ = ES == 2 ? 2 : 1; // matrix-core steps of a k step of 128 bytes
+
+// A barrier of the workgroup that the compiler moves no memory access across; this wavefront's LDS accesses are through before it.
+__device__ __forceinline__ void barrier()
+{
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+__device__ __forceinline__ int clamp_to(int x, int high) { return x < 0 ? 0 : x > high ? high : x; }
+
+// The rows of expert e: offsets outside [0, total] count as the nearer end, and an end ahead of its start as no rows.
+struct range_t { int first, last; };
+__device__ __forceinline__ range_t rows_of(const int *offsets, int e, int total)
+{
+    const int first = clamp_to(offsets[e], total), last = clamp_to(offsets[e + 1], total);
+    return {first, last < first ? first : last};
+}
+
+// Tiles of `bm` rows of the experts up to and including e, for all of them, into `table` (LDS): by the first wavefront, before a barrier.
+// Offsets that decrease make ranges overlap: the callers check what they find.
+__device__ __forceinline__ void count_tiles(const int *offsets, int experts, int total, int bm, int lane, int *table)
+{
+    int before = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        int n = 0;
+        if (e < experts) {
+            const range_t r = rows_of(offsets, e, total);
+            n = (r.last - r.first + bm - 1) / bm;
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __builtin_amdgcn_ds_bpermute((lane - d) * 4, n);
+            n += lane >= d ? x : 0;
+        }
+        n += before;
+        if (e < experts) table[e] = n;
+        before = __builtin_amdgcn_readlane(n, 63);
+    }
+}
+
+// Expert of row tile `t`, and which of the expert's tiles it is; all lanes of a wavefront together.
+struct tile_at { int expert, tile, tiles; };
+__device__ __forceinline__ tile_at find_tile(const int *table, int experts, int t, int lane)
+{
+    int e0 = 0;
+    for (;; e0 += 64) {
+        const int e = e0 + lane;
+        const bool behind = e < experts ? table[e] > t : true;
+        const unsigned long m = __ballot(behind);
+        if (m) {
+            int e1 = e0 + __builtin_ctzl(m);
+            e1 = e1 < experts ? e1 : experts - 1;
+            const int from = e1 ? table[e1 - 1] : 0, to = table[e1];
+            return {__builtin_amdgcn_readfirstlane(e1), __builtin_amdgcn_readfirstlane(t - from), __builtin_amdgcn_readfirstlane(to - from)};
+        }
+    }
+}
+
+// 4 bytes per lane from a buffer to `dst` (wave-uniform) + 4 * lane; as gather_lds16 in common.h
+__device__ __forceinline__ void gather_lds4(const rsrc_t &buffer, unsigned voff, unsigned dst)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(uniform(dst)), "v"(voff), "s"(buffer) : "memory", "m0");
+}
+__device__ __forceinline__ void gather_lds16_at(const rsrc_t &buffer, unsigned voff, unsigned soff, unsigned dst)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
+                 : : "s"(uniform(dst)), "v"(voff), "s"(buffer), "s"(uniform(soff)) : "memory", "m0");
+}
+// this wavefront's LDS accesses are through, and none behind is moved ahead
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// up to four results of a row at `dst`, the first `n` of them
+__device__ __forceinline__ void store4(char *dst, f4_t x, int n)
+{
+    struct __attribute__((packed, aligned(sizeof(out_t)))) quad { out_t v[4]; };
+    quad q;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) q.v[i] = from_acc(x[i]);
+    if (n >= 4) {
+        *reinterpret_cast<quad *>(dst) = q;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+            if (i < n) reinterpret_cast<out_t *>(dst)[i] = q.v[i];
+    }
+}

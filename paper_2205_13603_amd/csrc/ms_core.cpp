@@ -113,6 +113,10 @@ const char *op_kind_name(int32_t kind)
     case MS_OP_DWCONV2D_NHWC: return "dwconv2d_nhwc";
     case MS_OP_SOFTMAX: return "softmax";
     case MS_OP_NORM: return "norm";
+    case MS_OP_RMS_NORM: return "rms_norm";
+    case MS_OP_SCALED_GEMM: return "scaled_gemm";
+    case MS_OP_GROUPED_GEMM: return "grouped_gemm";
+    case MS_OP_GROUPED_WGRAD: return "grouped_wgrad";
     default: return "?";
     }
 }
@@ -181,12 +185,95 @@ static int64_t conv_out(int64_t in, int64_t k, int64_t s, int64_t p)
     return span < 0 ? 0 : span / s + 1;
 }
 
+// Layers of language models: the operator in *op, its dims and types checked.
+static int32_t create_layer(const ms_op_desc &d, ms_op *op)
+{
+    const int ndims = d.kind == MS_OP_RMS_NORM || d.kind == MS_OP_SCALED_GEMM ? 3 : 4;
+    for (int i = 0; i < ndims; ++i) {
+        const bool eps = d.kind == MS_OP_RMS_NORM && i == 2; // may be zero, and any number of units up to 1
+        if (d.dims[i] < (eps ? 0 : 1) || d.dims[i] > (eps ? (int64_t)1000000000000 : int64_t(1) << 30))
+            return fail(MS_ERR_BAD_ARG, "ms_op_create: dims[%d] = %" PRId64 " out of range", i, d.dims[i]);
+    }
+    for (int i = ndims; i < 8; ++i)
+        if (d.dims[i]) return fail(MS_ERR_BAD_ARG, "ms_op_create: %s has %d dims, dims[%d] = %" PRId64, op_kind_name(d.kind), ndims, i, d.dims[i]);
+    if (d.stride || d.pad || d.relu || d.dilation || (d.has_bias && d.kind != MS_OP_RMS_NORM))
+        return fail(MS_ERR_BAD_ARG, "ms_op_create: stride/pad/bias/relu/dilation do not apply to %s", op_kind_name(d.kind));
+    if (d.has_bias != 0 && d.has_bias != 1) return fail(MS_ERR_BAD_ARG, "ms_op_create: has_bias = %d", d.has_bias);
+    if (!dtype_size(d.in_dtype) || !dtype_size(d.out_dtype)) return fail(MS_ERR_BAD_ARG, "ms_op_create: bad dtype %d or %d", d.in_dtype, d.out_dtype);
+    const bool half = d.in_dtype == MS_F16 || d.in_dtype == MS_BF16, f8 = d.in_dtype == MS_F8E4M3;
+    bool ok;
+    if (d.kind == MS_OP_RMS_NORM) ok = (half || d.in_dtype == MS_F32) && (d.out_dtype == d.in_dtype || d.out_dtype == MS_F8E4M3);
+    else if (f8) ok = d.kind != MS_OP_GROUPED_WGRAD && (d.out_dtype == MS_F16 || d.out_dtype == MS_BF16 || d.out_dtype == MS_F32);
+    else ok = d.kind != MS_OP_SCALED_GEMM && half && (d.out_dtype == d.in_dtype || d.out_dtype == MS_F32);
+    if (!ok)
+        return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s with in %s -> out %s is not supported", op_kind_name(d.kind), dtype_name(d.in_dtype), dtype_name(d.out_dtype));
+    for (int i = 0; i < 3; ++i)
+        if (d.a_strides[i] < 0 || d.b_strides[i] < 0) return fail(MS_ERR_BAD_ARG, "ms_op_create: negative stride");
+    op->d = d;
+    op->nb = 1;
+    op->in_size = dtype_size(d.in_dtype);
+    op->out_size = dtype_size(d.out_dtype);
+    int64_t *a = op->d.a_strides, *b = op->d.b_strides;
+    const bool a_zero = !a[0] && !a[1] && !a[2], b_zero = !b[0] && !b[1] && !b[2];
+    const int64_t es = op->in_size, most_row = MS_MAX_ROW_BYTES / es;
+    if (d.kind == MS_OP_RMS_NORM) {
+        op->M = d.dims[0];
+        op->K = d.dims[1];
+        op->N = 1;
+        if (a_zero) a[1] = op->K, a[2] = 1;
+        if (!b_zero || a[0] || a[2] != 1 || a[1] < op->K) return fail(MS_ERR_BAD_ARG, "ms_op_create: rms_norm takes a_strides {0, at least N, 1} and no b_strides");
+        if (a[1] > int64_t(1) << 30 || op->M * op->K > int64_t(1) << 40) return fail(MS_ERR_BAD_ARG, "ms_op_create: tensor too large");
+        return MS_OK;
+    }
+    const int o = d.kind == MS_OP_SCALED_GEMM ? 0 : 2;
+    if (o) op->nb = d.dims[0];
+    if (op->nb > MS_MAX_EXPERTS) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %" PRId64 " experts, at most %d", op->nb, MS_MAX_EXPERTS);
+    if (d.kind == MS_OP_GROUPED_WGRAD) {
+        op->K = d.dims[1];
+        op->M = d.dims[2];
+        op->N = d.dims[3];
+        if (a_zero) a[1] = 1, a[2] = op->M;
+        if (b_zero) b[1] = op->N, b[2] = 1;
+        if (a[1] != 1 || b[2] != 1 || a[2] < op->M || b[1] < op->N)
+            return fail(MS_ERR_UNSUPPORTED, "ms_op_create: grouped_wgrad takes rows of contiguous elements that do not overlap");
+        if (a[2] > most_row || b[1] > most_row) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: rows of more than %d bytes", MS_MAX_ROW_BYTES);
+    } else {
+        op->M = d.dims[o ? 1 : 0];
+        op->N = d.dims[o ? 2 : 1];
+        op->K = d.dims[o ? 3 : 2];
+        if (a_zero) a[1] = op->K, a[2] = 1;
+        if (b_zero) b[0] = op->N * op->K, b[1] = 1, b[2] = op->K;
+        const bool by_k = b[1] == 1 && b[2] >= op->K, by_j = b[2] == 1 && b[1] >= op->N;
+        if (a[2] != 1 || a[1] < op->K) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s takes rows of A contiguous along k that do not overlap", op_kind_name(d.kind));
+        if (!by_k && (!by_j || f8)) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s takes B contiguous along k%s, its rows not overlapping", op_kind_name(d.kind), f8 ? "" : " or j");
+        if (op->nb > 1 && b[0] < (by_k ? (op->N - 1) * b[2] + op->K : (op->K - 1) * b[1] + op->N)) return fail(MS_ERR_BAD_ARG, "ms_op_create: matrices of B overlap");
+        if (a[1] > most_row || (by_k ? b[2] : b[1]) > most_row || (by_k ? op->K : op->N) > most_row)
+            return fail(MS_ERR_UNSUPPORTED, "ms_op_create: rows of more than %d bytes", MS_MAX_ROW_BYTES);
+    }
+    a[0] = 0;
+    const double most = 1099511627776.0; // 2^40 elements
+    if ((double)op->M * op->N * (d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1) > most || (double)op->nb * b[0] > most || (double)op->N * op->K * op->nb > most ||
+        (double)op->M * op->K > most)
+        return fail(MS_ERR_BAD_ARG, "ms_op_create: tensor too large");
+    return MS_OK;
+}
+
 extern "C" int32_t ms_op_create(const ms_op_desc *desc, ms_op **out)
 {
     if (!desc || !out) return fail(MS_ERR_BAD_ARG, "ms_op_create: NULL argument");
     *out = nullptr;
     ms_op op;
     memset(&op, 0, sizeof op);
+    if (is_layer(desc->kind)) {
+        op.depth = op.kd = op.OD = 1;
+        const int32_t rc = create_layer(*desc, &op);
+        if (rc != MS_OK) return rc;
+        op.user = op.d;
+        ms_op *p = new (std::nothrow) ms_op(op);
+        if (!p) return fail(MS_ERR_NOMEM, "ms_op_create: out of memory");
+        *out = p;
+        return MS_OK;
+    }
     ms_op_desc conv = *desc;
     const bool is_1d = desc->kind == MS_OP_CONV1D_NWC;
     if (is_1d) {
@@ -386,6 +473,17 @@ extern "C" int32_t ms_op_loops(const ms_op *op, ms_loop *loops, int32_t *n_loops
         set_loop(&loops[n++], "i", op->M, 0); // b
         set_loop(&loops[n++], "k", op->K, 1); // fuse(m, n)
         break;
+    case MS_OP_RMS_NORM:
+        set_loop(&loops[n++], "i", op->M, 0);
+        set_loop(&loops[n++], "k", op->K, 1); // n: reduced for the sum of squares and the scales, then revisited for the output
+        break;
+    case MS_OP_GROUPED_WGRAD: set_loop(&loops[n++], "e", op->nb, 0); /* fallthrough */
+    case MS_OP_SCALED_GEMM:
+    case MS_OP_GROUPED_GEMM: // an expert's rows are a part of i; of k in the gradient, where it is the longest possible
+        set_loop(&loops[n++], "i", op->M, 0);
+        set_loop(&loops[n++], "j", op->N, 0);
+        set_loop(&loops[n++], "k", op->K, 1);
+        break;
     }
     *n_loops = n;
     return MS_OK;
@@ -426,6 +524,31 @@ extern "C" int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx, int64_t *byt
     case MS_OP_NORM:
         if (idx < 0) e = op->M;
         else if (idx == 0) e = op->M * op->K;
+        break;
+    case MS_OP_RMS_NORM:
+        if (idx == -1) e = op->M * op->K;
+        else if (idx == -2) sz = 4, e = d.out_dtype == MS_F8E4M3 ? op->M * scale_blocks(op->K) : 0;
+        else if (idx == -3) sz = op->in_size, e = d.has_bias ? op->M * op->K : 0;
+        else if (idx == 0) e = (op->M - 1) * d.a_strides[1] + op->K;
+        else if (idx == 1) e = op->K;
+        else if (idx == 2 && d.has_bias) e = op->M * op->K;
+        break;
+    case MS_OP_SCALED_GEMM:
+    case MS_OP_GROUPED_GEMM: {
+        const int at = d.kind == MS_OP_SCALED_GEMM ? 2 : 3; // of the scales
+        if (idx == -1) e = op->M * op->N;
+        else if (idx == 0) e = (op->M - 1) * d.a_strides[1] + op->K;
+        else if (idx == 1) e = (op->nb - 1) * d.b_strides[0] + (op->K - 1) * d.b_strides[1] + (op->N - 1) * d.b_strides[2] + 1;
+        else if (idx == 2 && at == 3) sz = 4, e = op->nb + 1;
+        else if (idx == at && d.in_dtype == MS_F8E4M3) sz = 4, e = op->M * scale_blocks(op->K);
+        else if (idx == at + 1 && d.in_dtype == MS_F8E4M3) sz = 4, e = op->nb * scale_blocks(op->N) * scale_blocks(op->K);
+        break;
+    }
+    case MS_OP_GROUPED_WGRAD:
+        if (idx == -1) e = op->nb * op->M * op->N;
+        else if (idx == 0) e = (op->K - 1) * d.a_strides[2] + op->M;
+        else if (idx == 1) e = (op->K - 1) * d.b_strides[1] + op->N;
+        else if (idx == 2) sz = 4, e = op->nb + 1;
         break;
     }
     if (e < 0) return fail(MS_ERR_BAD_ARG, "ms_op_tensor_bytes: no tensor %d", idx);
@@ -472,6 +595,26 @@ extern "C" int32_t ms_op_work(const ms_op *op, double *flop, double *bytes)
         f = 2.0 * op->M * op->K;
         b = (double)op->M * op->K * op->in_size + (double)op->M * op->out_size;
         break;
+    case MS_OP_RMS_NORM: {
+        // per element: square, add, two products; the residual's addition; maximum, product and rounding of an 8-bit output
+        const double e = (double)op->M * op->K;
+        f = e * (4 + (d.has_bias ? 1 : 0) + (d.out_dtype == MS_F8E4M3 ? 3 : 0));
+        b = e * (op->in_size * (d.has_bias ? 3 : 1) + op->out_size) + (double)op->K * op->in_size;
+        if (d.out_dtype == MS_F8E4M3) b += 4.0 * op->M * scale_blocks(op->K);
+        break;
+    }
+    case MS_OP_SCALED_GEMM:
+    case MS_OP_GROUPED_GEMM:
+        // as if every row had an expert and every expert a row
+        f = 2.0 * op->M * op->N * op->K;
+        b = ((double)op->M * op->K + (double)op->nb * op->N * op->K) * op->in_size + (double)op->M * op->N * op->out_size;
+        if (d.in_dtype == MS_F8E4M3) b += 4.0 * scale_blocks(op->K) * ((double)op->M + (double)op->nb * scale_blocks(op->N));
+        if (d.kind == MS_OP_GROUPED_GEMM) b += 4.0 * (op->nb + 1);
+        break;
+    case MS_OP_GROUPED_WGRAD:
+        f = 2.0 * op->M * op->N * op->K;
+        b = (double)op->K * (op->M + op->N) * op->in_size + (double)op->nb * op->M * op->N * op->out_size + 4.0 * (op->nb + 1);
+        break;
     }
     *flop = f;
     *bytes = b;
@@ -513,6 +656,15 @@ extern "C" int32_t ms_space_describe(const ms_op *op, uint32_t flags, ms_space *
     if (!op || !out) return fail(MS_ERR_BAD_ARG, "ms_space_describe: NULL argument");
     memset(out, 0, sizeof *out);
     const ms_op_desc &d = op->d;
+    if (is_layer(d.kind)) { // no module changes their kernels; the one decision is what a workgroup works on
+        out->family = d.kind == MS_OP_RMS_NORM ? MS_FAM_RMS_NORM : MS_FAM_RAGGED;
+        if (d.kind == MS_OP_RMS_NORM) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
+        else add_cat(out, MS_SLOT_BLOCK, "block", {0, 16016, 16032, 32032, 64032, 64128, 128128, 256256});
+        ms_slot &s = out->slots[0];
+        for (int c = 1; c < s.n_candidates; ++c)
+            if (!layer_block_fits(op, s.candidates[c])) s.weight[c] = 0;
+        return MS_OK;
+    }
     if (flags & 0x80000000u) flags &= 0xffu; // all-ones masks of earlier records: the default set, opt-in modules off
     if (d.in_dtype == MS_F32 && !((flags & MS_SPACE_TENSORIZE_F32) && d.kind != MS_OP_DWCONV2D_NHWC && !is_conv2d(d.kind)))
         flags &= ~(MS_SPACE_TENSORIZE | MS_SPACE_TENSORIZE_F32);
@@ -1052,6 +1204,19 @@ extern "C" int32_t ms_trace_to_text(const ms_op *op, const ms_space *space, cons
         if (p.body == MS_BODY_PHASES) appendf(s, "# body=phases: i in the order of the %d output phases, k0 over the taps of a tile's phase only\n", p.body_tile);
         if (p.body == MS_BODY_CONV_STEPS) appendf(s, "# body=conv-steps: %d pixels x %d channels per workgroup, this operator's own split\n", p.block_m, p.block_n);
         if (p.body == MS_BODY_DOUBLE_STEPS) appendf(s, "# body=double-steps: two k0 steps per LDS stage, %d stages\n", p.body_tile);
+        if (is_layer_family(p.family)) {
+            if (p.body == MS_BODY_RMS_ROWS) appendf(s, "# body=rms-rows: %d wavefronts share a row, which stays in their registers\n", p.body_tile);
+            else appendf(s, "# body=%s: %d rows of one expert x %d columns per workgroup, the last of each masked\n",
+                         p.body == MS_BODY_RAGGED_ROWS ? "ragged-rows" : "ragged-tiles", p.block_m, p.block_n);
+            appendf(s, "# sizes are arguments of the kernel; workgroup=%d threads, grid=%d, lds=%d B\n", p.threads, p.grid[0], p.lds_bytes);
+            if (needed) *needed = s.size() + 1;
+            if (buf && cap) {
+                const size_t n = std::min(cap - 1, s.size());
+                memcpy(buf, s.data(), n);
+                buf[n] = 0;
+            }
+            return MS_OK;
+        }
         if (p.mfma && !image_rows) appendf(s, "tensorize(block=C, intrin=mfma_%dx%dx%d)\n", p.tile_unit[0], p.tile_unit[1], p.tile_unit[2]);
         const char *nm[4] = {"i", "j", "c", "k"};
         const int32_t *tl[4] = {p.ti, p.tj, p.tc, p.tk};
@@ -1175,6 +1340,22 @@ extern "C" int32_t ms_trace_from_text(const ms_space *space, const char *text, m
     }
     if (pos != space->n_slots) return fail(MS_ERR_INVALID_TRACE, "ms_trace_from_text: truncated trace: %d of %d sampling instructions", pos, space->n_slots);
     out->n = pos;
+    return MS_OK;
+}
+
+extern "C" int32_t ms_trace_default(const ms_space *space, ms_trace *out)
+{
+    if (!space_ok(space) || !out) return fail(MS_ERR_BAD_ARG, "ms_trace_default: bad argument");
+    memset(out, 0, sizeof *out);
+    for (int i = 0; i < space->n_slots; ++i) {
+        const ms_slot &s = space->slots[i];
+        if (s.slot_id != MS_SLOT_BLOCK || s.kind != MS_SLOT_CATEGORICAL || s.candidates[0] != 0)
+            return fail(MS_ERR_UNSUPPORTED, "ms_trace_default: no rule decides %s", s.name);
+        out->d[i].slot_id = s.slot_id;
+        out->d[i].kind = s.kind;
+        out->d[i].n = 1;
+    }
+    out->n = space->n_slots;
     return MS_OK;
 }
 

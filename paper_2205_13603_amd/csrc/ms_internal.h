@@ -30,6 +30,25 @@ inline bool follows_decisions(const ms_variant_params *p)
 {
     return p->body == MS_BODY_NEST || p->body == MS_BODY_PHASES || p->body == MS_BODY_DOUBLE_STEPS;
 }
+// Layers of language models: sizes are arguments of their kernels
+inline bool is_layer(int32_t kind) { return kind >= MS_OP_RMS_NORM && kind <= MS_OP_GROUPED_WGRAD; }
+inline bool is_layer_family(int32_t family) { return family == MS_FAM_RMS_NORM || family == MS_FAM_RAGGED; }
+inline int64_t scale_blocks(int64_t n) { return (n + 127) / 128; }
+// What a launch hands to the kernels of layers; the same structs stand in ragged.h and rms_norm.hip.  Rows and distances in bytes.
+struct RaggedArgs {
+    const void *a, *b, *offsets, *sa, *sb;
+    void *c;
+    int64_t a_row, b_row, b_expert;                 // of B and Q: rows of k values, or of columns where k runs along them
+    int64_t a_inst, b_inst, sa_inst, sb_inst, c_inst;
+    int32_t rows, cols, depth, experts;             // GROUPED_WGRAD: I, J, T, E
+};
+struct RmsArgs {
+    const void *x, *w, *r;
+    void *y, *s, *h;
+    int64_t x_row, x_inst; // in elements
+    int32_t rows, cols, instances;
+    float eps;
+};
 inline bool is_3d(const ms_op *op) { return op->depth > 1 || op->kd > 1; }
 
 // (m, n, k) of an MS_MFMA_CODE
@@ -66,6 +85,9 @@ const char *dtype_name(int32_t dt);
 const char *op_kind_name(int32_t kind);
 
 extern ms_limits g_limits;
+
+// Whether a workgroup of an operator on rows by expert, or of the norm of rows, can be what `code` says (MS_SLOT_BLOCK).
+bool layer_block_fits(const ms_op *op, int64_t code);
 
 // Kernel source generation: template file + "-D" defines for a variant.
 struct KernelSpec {

@@ -677,11 +677,145 @@ void resolve_body(const ms_op *op, ms_variant_params *p)
     p->waves = p->threads / 64;
 }
 
+// ---- layers of language models: kernels that take sizes as arguments, chosen by what a workgroup works on
+
+// B (the products) contiguous along k
+bool ragged_by_k(const ms_op *op) { return op->d.kind != MS_OP_GROUPED_WGRAD && op->d.b_strides[1] == 1 && op->d.b_strides[2] >= op->K; }
+
+// loads of 16 bytes: rows and extents of whole 16 bytes
+bool ragged_aligned(const ms_op *op)
+{
+    const ms_op_desc &d = op->d;
+    const int64_t n = 16 / op->in_size;
+    if (d.kind == MS_OP_GROUPED_WGRAD) return !(op->M % n || op->N % n || d.a_strides[2] % n || d.b_strides[1] % n);
+    if (op->K % n || d.a_strides[1] % n || (op->nb > 1 && d.b_strides[0] % n)) return false;
+    return ragged_by_k(op) ? d.b_strides[2] % n == 0 : op->N % n == 0 && d.b_strides[1] % n == 0;
+}
+
+struct RaggedTile {
+    int bm, bn, wi, wj, stages; // tiles in LDS: wavefronts by rows and columns; few rows: wi = wavefronts that share the reduction
+    bool few;
+    int64_t lds;
+};
+// The tile that an MS_SLOT_BLOCK code names; its LDS as the kernels lay it out.
+RaggedTile ragged_tile(const ms_op *op, int64_t code)
+{
+    RaggedTile t;
+    t.bm = (int)(code / 1000);
+    t.bn = (int)(code % 1000);
+    t.few = t.bn <= 32;
+    const bool scaled = op->in_size == 1, table = op->d.kind == MS_OP_GROUPED_GEMM;
+    if (t.few) {
+        t.wi = 4;
+        t.wj = 1;
+        t.stages = t.bm + t.bn > 64 ? 2 : 4;
+        const int64_t ring = (int64_t)t.wi * t.stages * ((t.bm + t.bn) * 128 + (scaled ? 512 : 0));
+        t.lds = std::max<int64_t>(ring, (int64_t)t.wi * t.bm * t.bn * 4) + (table ? 4096 : 0);
+    } else {
+        t.wi = 2;
+        t.wj = code == 256256 ? 4 : 2;
+        t.stages = code == 64128 ? 3 : 2;
+        t.lds = (int64_t)t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
+    }
+    return t;
+}
+// row tiles of a launch: of every expert the last may be a part of one
+int64_t ragged_row_tiles(const ms_op *op, int64_t bm)
+{
+    const int64_t experts = op->d.kind == MS_OP_GROUPED_GEMM ? std::min(op->nb, op->M) : 1;
+    return op->d.kind == MS_OP_GROUPED_GEMM ? (op->M - experts) / bm + experts : (op->M + bm - 1) / bm;
+}
+int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
+{
+    return ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) * (op->d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1);
+}
+
+int64_t ragged_rule(const ms_op *op)
+{
+    if (!ragged_aligned(op)) return 64128;
+    if (op->d.kind == MS_OP_GROUPED_WGRAD) return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 ? 256256 : 128128;
+    const int64_t rows = op->d.kind == MS_OP_GROUPED_GEMM ? (op->M + op->nb - 1) / op->nb : op->M; // of an expert
+    if (ragged_by_k(op)) {
+        if (rows <= 16) return 16032;
+        if (rows <= 32) return 32032;
+    }
+    if (rows <= 64) return 64128;
+    return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 && rows >= 192 ? 256256 : 128128;
+}
+
+int64_t rms_rule(const ms_op *op)
+{
+    // few rows: a chunk of 8 columns for every lane; many: the four that its registers hold
+    const int64_t chunk = op->M <= 512 ? 512 : 2048;
+    int64_t waves = 1;
+    while (waves < 16 && waves * chunk < op->K) waves *= 2;
+    return waves;
+}
+
+// fields of a layer's variant; the limits are checked
+int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *trace, ms_variant_params *p)
+{
+    int64_t code = cat_value(space, trace, MS_SLOT_BLOCK, 0);
+    if (space->family != (op->d.kind == MS_OP_RMS_NORM ? MS_FAM_RMS_NORM : MS_FAM_RAGGED)) return fail(MS_ERR_BAD_ARG, "ms_trace_validate: the space is another operator's");
+    if (code && !layer_block_fits(op, code)) return reject("block: this operator has no kernel for %" PRId64, code);
+    p->grid[1] = p->grid[2] = 1;
+    p->rfactor = 1;
+    p->tile_unit[0] = p->tile_unit[1] = p->tile_unit[2] = 1;
+    int64_t grid;
+    if (op->d.kind == MS_OP_RMS_NORM) {
+        if (!code) code = rms_rule(op);
+        p->body = MS_BODY_RMS_ROWS;
+        p->waves = std::max(4, (int)code);
+        p->threads = p->waves * 64;
+        p->block_m = p->waves / (int)code;
+        p->block_n = 1;
+        p->block_k = (int32_t)code * 512;
+        p->vec = 8;
+        p->acc_per_thread = 32;
+        p->lds_bytes = 2 * p->waves * 4;
+        grid = (op->M + p->block_m - 1) / p->block_m;
+    } else {
+        const bool aligned = ragged_aligned(op);
+        if (!code) code = ragged_rule(op);
+        const RaggedTile t = ragged_tile(op, code);
+        p->body = t.few ? MS_BODY_RAGGED_ROWS : MS_BODY_RAGGED_TILES;
+        p->block_m = t.bm;
+        p->block_n = t.bn;
+        p->block_k = 128 / op->in_size;
+        p->waves = t.wi * t.wj;
+        p->threads = p->waves * 64;
+        p->tile_unit[0] = p->tile_unit[1] = 16;
+        p->tile_unit[2] = op->in_size == 1 ? 128 : 32;
+        p->mfma = MS_MFMA_CODE(16, 16, p->tile_unit[2]);
+        p->acc_per_thread = t.few ? t.bm * t.bn / 64 : t.bm * t.bn / p->threads;
+        p->vec = p->vec_b = aligned ? 16 / op->in_size : 1;
+        p->lds_bytes = (int32_t)t.lds;
+        grid = ragged_tiles(op, t);
+    }
+    if (grid > 0x7fffffff || (p->family == MS_FAM_RAGGED && grid * p->threads > 0xffffffffll)) return reject("grid of %" PRId64 " workgroups overflows", grid);
+    p->grid[0] = (int32_t)grid;
+    p->body_tile = (int32_t)code;
+    if (p->threads > g_limits.max_threads || p->waves > g_limits.max_waves) return reject("%d threads per workgroup, the limit is %d", p->threads, g_limits.max_threads);
+    if (p->lds_bytes > g_limits.max_lds_bytes) return reject("%d bytes of LDS, the limit is %d", p->lds_bytes, g_limits.max_lds_bytes);
+    if (p->acc_per_thread > g_limits.max_acc_per_thread) return reject("%d accumulators per lane, the register budget is %d", p->acc_per_thread, g_limits.max_acc_per_thread);
+    return MS_OK;
+}
+
 uint64_t hash_params(const ms_op *op, const ms_variant_params *p)
 {
     uint64_t h = 0x243F6A8885A308D3ull;
     auto add = [&](uint64_t v) { h = mix64(h ^ mix64(v)); };
     const ms_op_desc &d = op->d;
+    if (is_layer_family(p->family)) { // sizes do not select code
+        add(0x1A7E4000000ull + (uint64_t)d.kind);
+        add((uint64_t)d.in_dtype);
+        add((uint64_t)d.out_dtype);
+        add((uint64_t)d.has_bias);
+        add((uint64_t)ragged_by_k(op));
+        add((uint64_t)p->body_tile);
+        add((uint64_t)p->vec);
+        return h;
+    }
     add((uint64_t)d.kind);
     add((uint64_t)d.in_dtype);
     add((uint64_t)d.out_dtype);
@@ -793,6 +927,14 @@ extern "C" int32_t ms_trace_validate(const ms_op *op, const ms_space *space, con
     p.family = space->family;
     const ms_op_desc &d = op->d;
     const ms_limits &L = g_limits;
+    if (is_layer(d.kind) || is_layer_family(p.family)) {
+        if (!is_layer(d.kind)) return fail(MS_ERR_BAD_ARG, "ms_trace_validate: the space is another operator's");
+        const int32_t rc = resolve_layer(op, space, trace, &p);
+        if (rc != MS_OK) return rc;
+        p.key = hash_params(op, &p);
+        if (out) *out = p;
+        return MS_OK;
+    }
     p.unroll = (int32_t)cat_value(space, trace, MS_SLOT_UNROLL, 0);
     p.vec = (int32_t)cat_value(space, trace, MS_SLOT_VECTORIZE, 1);
     p.vec_b = (int32_t)cat_value(space, trace, MS_SLOT_VECTORIZE_B, 1);
@@ -1303,6 +1445,15 @@ int32_t ms::validate_as_nest(const ms_op *op, const ms_space *space, const ms_tr
     return rc;
 }
 
+bool ms::layer_block_fits(const ms_op *op, int64_t code)
+{
+    if (op->d.kind == MS_OP_RMS_NORM) return code >= 1 && code <= 16 && (code & (code - 1)) == 0;
+    const bool few = code % 1000 <= 32;
+    if (!ragged_aligned(op)) return code == 64128;
+    if (few) return ragged_by_k(op) && (code == 16016 || code == 16032 || code == 32032 || code == 64032);
+    return code == 64128 || code == 128128 || code == 256256;
+}
+
 namespace ms {
 
 static std::string def(const char *name, int64_t v)
@@ -1354,6 +1505,33 @@ int32_t make_kernel_spec(const ms_op *op, const ms_variant_params *p, KernelSpec
     auto &D = k.defines;
     D.push_back(def("IN_DT", dt_code(d.in_dtype)));
     D.push_back(def("OUT_DT", dt_code(d.out_dtype)));
+    if (p->family == MS_FAM_RMS_NORM) {
+        D.push_back(def("WAVES", p->body_tile));
+        D.push_back(def("RESIDUAL", d.has_bias));
+        k.template_name = "rms_norm.hip";
+        *out = k;
+        return MS_OK;
+    }
+    if (p->family == MS_FAM_RAGGED) {
+        const RaggedTile t = ragged_tile(op, p->body_tile);
+        const bool wgrad = d.kind == MS_OP_GROUPED_WGRAD;
+        D.push_back(def("GROUPED", d.kind != MS_OP_SCALED_GEMM));
+        D.push_back(def("BM", t.bm));
+        D.push_back(def("BN", t.bn));
+        D.push_back(def("WI", t.wi));
+        D.push_back(def("STAGES", t.stages));
+        D.push_back(def("LDS_HOST", t.lds));
+        if (!t.few) {
+            D.push_back(def("WGRAD", wgrad));
+            D.push_back(def("A_KC", !wgrad));
+            D.push_back(def("B_KC", ragged_by_k(op)));
+            D.push_back(def("WJ", t.wj));
+            D.push_back(def("ALIGNED", p->vec > 1));
+        }
+        k.template_name = t.few ? "gemm_ragged_rows.hip" : "gemm_ragged.hip";
+        *out = k;
+        return MS_OK;
+    }
     const bool conv_patch = p->body == MS_BODY_CONV_PATCH, conv_steps = p->body == MS_BODY_CONV_STEPS;
     if (follows_decisions(p) || conv_steps) push_schedule(D, p);
     if (p->family == MS_FAM_GEMM_ALU || p->family == MS_FAM_GEMM_MFMA) {
@@ -1580,6 +1758,16 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
     if (out_elems != ob / op->out_size) return fail(MS_ERR_BAD_ARG, "ms_variant_coverage: out_elems %" PRId64 " != %" PRId64, out_elems, ob / op->out_size);
     memset(counts, 0, sizeof(int32_t) * (size_t)out_elems);
     const ms_op_desc &d = op->d;
+    if (is_layer_family(p->family)) {
+        // rows and columns behind the last are masked; of a grouped product all rows taken for one expert's
+        const int64_t rows = op->M, cols = d.kind == MS_OP_RMS_NORM ? op->K : op->N, bn = d.kind == MS_OP_RMS_NORM ? cols : p->block_n;
+        for (int64_t e = 0; e < (d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1); ++e)
+            for (int64_t i0 = 0; i0 < rows; i0 += p->block_m)
+                for (int64_t j0 = 0; j0 < cols; j0 += bn)
+                    for (int64_t i = i0; i < std::min(rows, i0 + p->block_m); ++i)
+                        for (int64_t j = j0; j < std::min(cols, j0 + bn); ++j) ++counts[(e * rows + i) * cols + j];
+        return MS_OK;
+    }
     if (p->body == MS_BODY_IMAGE_ROWS) {
         const ConvRows c = conv_rows_tiles(op, p->body_tile);
         const int64_t bn = c.tn * 32, jbs = op->N / bn, ohw = op->OH * op->OW;
@@ -1702,6 +1890,15 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
 extern "C" int32_t ms_variant_reduction_coverage(const ms_op *op, const ms_variant_params *p, int32_t *counts, int64_t k_elems, int64_t *needed)
 {
     if (!op || !p) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
+    if (is_layer_family(p->family)) { // steps of block_k from the first k on, masked behind the last
+        if (needed) *needed = op->K;
+        if (!counts) return needed ? MS_OK : fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
+        if (k_elems != op->K) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: k_elems %" PRId64 " != %" PRId64, k_elems, op->K);
+        memset(counts, 0, sizeof(int32_t) * (size_t)k_elems);
+        for (int64_t k0 = 0; k0 < op->K; k0 += p->block_k)
+            for (int64_t k = k0; k < std::min(op->K, k0 + p->block_k); ++k) ++counts[k];
+        return MS_OK;
+    }
     const bool dw = p->family == MS_FAM_DWCONV;
     const int unit = dw ? 1 : std::max(1, p->tile_unit[2]);
     const bool masked = p->body == MS_BODY_ROW_VECTORS || p->body == MS_BODY_IMAGE_ROWS || p->body == MS_BODY_CONV_STEPS; // positions beyond K are left out

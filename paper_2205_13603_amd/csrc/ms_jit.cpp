@@ -108,6 +108,13 @@ static int32_t get_source(const std::string &name, const Source **src) // entrie
     std::string marker = "#include \"common.h\"";
     size_t at = body.find(marker);
     if (at != std::string::npos) body.replace(at, marker.size(), common);
+    marker = "#include \"ragged.h\""; // of the products over rows by expert
+    at = body.find(marker);
+    if (at != std::string::npos) {
+        std::string shared;
+        if (!read_file(dir + "/ragged.h", &shared)) return fail(MS_ERR_COMPILE, "kernel header %s/ragged.h not found", dir.c_str());
+        body.replace(at, marker.size(), shared);
+    }
     const uint64_t hash = hash_bytes(body);
     std::lock_guard<std::mutex> lk(g_mu);
     *src = &g_sources.emplace(name, Source{body, hash}).first->second;

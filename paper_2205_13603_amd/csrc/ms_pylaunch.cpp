@@ -35,27 +35,33 @@ PyObject *bind(PyObject *, PyObject *address)
     Py_RETURN_NONE;
 }
 
-// launch(variant, inputs, output, instances, stream, workspace) -> status code
+// launch(variant, inputs, output or sequence of outputs, instances, stream, workspace) -> status code
 PyObject *launch(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != 6 || !g_launch) {
         PyErr_SetString(PyExc_TypeError, "launch(variant, inputs, output, instances, stream, workspace) after bind()");
         return nullptr;
     }
-    void *variant, *in[4] = {nullptr, nullptr, nullptr, nullptr}, *out, *stream, *workspace;
-    PyObject *seq = PySequence_Fast(args[1], "inputs: a sequence of device pointers");
-    if (!seq) return nullptr;
-    const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
-    bool ok = count <= 4;
-    if (!ok) PyErr_Format(PyExc_ValueError, "%zd inputs, an operator has at most 4", count);
-    for (Py_ssize_t i = 0; ok && i < count; ++i) ok = pointer(PySequence_Fast_GET_ITEM(seq, i), &in[i]);
-    Py_DECREF(seq);
-    if (!ok || !pointer(args[0], &variant) || !pointer(args[2], &out) || !pointer(args[4], &stream) || !pointer(args[5], &workspace)) return nullptr;
+    constexpr Py_ssize_t MOST = 8; // tensors a side
+    void *variant, *in[MOST] = {}, *out[MOST] = {}, *stream, *workspace;
+    auto tensors = [](PyObject *o, const char *what, void **to) {
+        PyObject *seq = PySequence_Fast(o, what);
+        if (!seq) return false;
+        const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
+        bool ok = count <= MOST;
+        if (!ok) PyErr_Format(PyExc_ValueError, "%zd tensors, an operator has at most %zd", count, MOST);
+        for (Py_ssize_t i = 0; ok && i < count; ++i) ok = pointer(PySequence_Fast_GET_ITEM(seq, i), &to[i]);
+        Py_DECREF(seq);
+        return ok;
+    };
+    const bool several = PyList_Check(args[2]) || PyTuple_Check(args[2]);
+    if (!tensors(args[1], "inputs: a sequence of device pointers", in) ||
+        !(several ? tensors(args[2], "outputs: a sequence of device pointers", out) : pointer(args[2], out)) || !pointer(args[0], &variant) || !pointer(args[4], &stream) || !pointer(args[5], &workspace)) return nullptr;
     const int32_t instances = (int32_t)PyLong_AsUnsignedLongMask(args[3]);
     if (PyErr_Occurred()) return nullptr;
     int32_t rc;
     Py_BEGIN_ALLOW_THREADS // the queue of a stream may be full
-    rc = g_launch(variant, in, &out, workspace, instances, stream);
+    rc = g_launch(variant, in, out, workspace, instances, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
 }

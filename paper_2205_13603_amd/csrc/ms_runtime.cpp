@@ -7,6 +7,7 @@
 #include <algorithm>
 #include <atomic>
 #include <cstring>
+#include <map>
 #include <mutex>
 #include <new>
 #include <string>
@@ -237,8 +238,10 @@ extern "C" int32_t ms_prebuild(const ms_op *op, const ms_space *space, const ms_
 
 // Loads the kernels of a variant on device `dev`, the current one: also that of few tiles, whichever a launch takes, so that a
 // variant that has been launched once loads nothing more on that device.
+static int32_t load_layer(ms_variant *v, int dev);
 static int32_t ensure_loaded(ms_variant *v, int dev)
 {
+    if (is_layer_family(v->p.family)) return load_layer(v, dev);
     for (ms_variant *second : {v->few, v->fill}) {
         const int32_t rc = second ? ensure_loaded(second, dev) : MS_OK;
         if (rc != MS_OK) return rc;
@@ -266,6 +269,125 @@ static int32_t ensure_loaded(ms_variant *v, int dev)
     if (v->spec.many_grid) HIP_TRY(hipModuleGetFunction(&v->fn_many, v->mod, (v->spec.entry + "_many").c_str()));
     v->device = dev;
     v->compute_units = prop.multiProcessorCount;
+    return MS_OK;
+}
+
+// Kernels of layers: one code object serves operators of all sizes, so it is loaded once for each device and stays until the process
+// ends; a variant only looks it up.  The variants of a decoding step's many sizes then cost no loading.
+struct LoadedKernel {
+    hipModule_t mod;
+    hipFunction_t fn;
+    int compute_units;
+};
+static std::mutex g_layers_mu;
+static std::map<std::pair<const std::vector<char> *, int>, LoadedKernel> g_layers;
+
+static int32_t load_layer(ms_variant *v, int dev)
+{
+    if (__atomic_load_n(&v->device, __ATOMIC_ACQUIRE) == dev) return MS_OK;
+    std::lock_guard<std::mutex> lk(g_layers_mu);
+    auto at = g_layers.find({v->code, dev});
+    if (at == g_layers.end()) {
+        hipDeviceProp_t prop;
+        HIP_TRY(hipGetDeviceProperties(&prop, dev));
+        if (strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+            return fail(MS_ERR_UNSUPPORTED, "device %d is %s; kernels are built for gfx950 only", dev, prop.gcnArchName);
+        if ((size_t)v->p.lds_bytes > prop.sharedMemPerBlock)
+            return fail(MS_ERR_HIP, "variant needs %d bytes of LDS, the device offers %zu per workgroup", v->p.lds_bytes, (size_t)prop.sharedMemPerBlock);
+        LoadedKernel k = {nullptr, nullptr, prop.multiProcessorCount};
+        HIP_TRY(hipModuleLoadData(&k.mod, v->code->data()));
+        const hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
+        if (e != hipSuccess) {
+            (void)hipModuleUnload(k.mod);
+            return fail(MS_ERR_HIP, "hipModuleGetFunction: %s", hipGetErrorString(e));
+        }
+        at = g_layers.emplace(std::make_pair(v->code, dev), k).first;
+    }
+    v->fn = at->second.fn;
+    v->compute_units = at->second.compute_units;
+    __atomic_store_n(&v->device, dev, __ATOMIC_RELEASE);
+    return MS_OK;
+}
+
+// Inputs and outputs of a layer in the order of ms_op_desc: how many, and which may be NULL.
+static int layer_inputs(const ms_op &op)
+{
+    const bool scaled = op.d.in_dtype == MS_F8E4M3;
+    switch (op.d.kind) {
+    case MS_OP_RMS_NORM: return 2 + op.d.has_bias;
+    case MS_OP_SCALED_GEMM: return 4;
+    case MS_OP_GROUPED_GEMM: return scaled ? 5 : 3;
+    default: return 3;
+    }
+}
+static bool layer_has_output(const ms_op &op, int i)
+{
+    return i == 0 || (op.d.kind == MS_OP_RMS_NORM && (i == 1 ? op.d.out_dtype == MS_F8E4M3 : i == 2 && op.d.has_bias));
+}
+
+static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *const *outputs, int32_t instances, void *stream)
+{
+    const ms_op &op = v->op;
+    const ms_op_desc &d = op.d;
+    const int ni = layer_inputs(op);
+    for (int i = 0; i < ni; ++i)
+        if (!inputs[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: inputs[%d] of %s is NULL", i, d.kind == MS_OP_RMS_NORM ? "the norm" : "the product");
+    for (int i = 0; i < (d.kind == MS_OP_RMS_NORM ? 3 : 1); ++i)
+        if (layer_has_output(op, i) && !outputs[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: outputs[%d] is NULL", i);
+    if (instances > 65535) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %d instances overflow the grid", instances);
+    auto aligned = [&](const void *p, int64_t to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; };
+    RaggedArgs g;
+    RmsArgs r;
+    void *args[1];
+    unsigned gx = v->spec.grid[0], gy = (unsigned)instances;
+    if (d.kind == MS_OP_RMS_NORM) {
+        const void *x = inputs[0], *w = inputs[1], *res = d.has_bias ? inputs[2] : nullptr;
+        void *s = d.out_dtype == MS_F8E4M3 ? outputs[1] : nullptr, *h = d.has_bias ? outputs[2] : nullptr;
+        if (!aligned(x, op.in_size) || !aligned(w, op.in_size) || !aligned(res, op.in_size) || !aligned(h, op.in_size) || !aligned(outputs[0], op.out_size) || !aligned(s, 4))
+            return fail(MS_ERR_BAD_ARG, "ms_variant_launch: a tensor is not aligned to its elements");
+        r = {x, w, res, outputs[0], s, h, d.a_strides[1], (op.M - 1) * d.a_strides[1] + op.K, (int32_t)op.M, (int32_t)op.K, instances, (float)((double)d.dims[2] * MS_EPS_UNIT)};
+        const int64_t groups = (op.M * instances + v->p.block_m - 1) / v->p.block_m;
+        gx = (unsigned)std::min<int64_t>(groups, 1 << 20); // workgroups go on to further rows
+        gy = 1;
+        args[0] = &r;
+    } else {
+        const int at = d.kind == MS_OP_SCALED_GEMM ? 2 : 3; // of the scales
+        const bool scaled = d.in_dtype == MS_F8E4M3, grouped = d.kind != MS_OP_SCALED_GEMM;
+        const void *offsets = grouped ? inputs[2] : nullptr, *sa = scaled ? inputs[at] : nullptr, *sb = scaled ? inputs[at + 1] : nullptr;
+        if (!aligned(inputs[0], 16) || !aligned(inputs[1], 16) || !aligned(outputs[0], 16))
+            return fail(MS_ERR_BAD_ARG, "ms_variant_launch: the product's tensors must be 16-byte aligned");
+        if (!aligned(offsets, 4) || !aligned(sa, 4) || !aligned(sb, 4)) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: offsets and scales must be 4-byte aligned");
+        memset(&g, 0, sizeof g);
+        g.a = inputs[0];
+        g.b = inputs[1];
+        g.c = outputs[0];
+        g.offsets = offsets;
+        g.sa = sa;
+        g.sb = sb;
+        const bool wgrad = d.kind == MS_OP_GROUPED_WGRAD, by_k = !wgrad && d.b_strides[1] == 1 && d.b_strides[2] >= op.K;
+        g.a_row = (wgrad ? d.a_strides[2] : d.a_strides[1]) * op.in_size;
+        g.b_row = (by_k ? d.b_strides[2] : d.b_strides[1]) * op.in_size;
+        g.b_expert = wgrad ? 0 : d.b_strides[0] * op.in_size;
+        int64_t bytes[5] = {0, 0, 0, 0, 0};
+        for (int i = 0; i < ni; ++i) (void)ms_op_tensor_bytes(&op, i, &bytes[i]);
+        (void)ms_op_tensor_bytes(&op, -1, &g.c_inst);
+        g.a_inst = bytes[0];
+        g.b_inst = bytes[1];
+        g.sa_inst = scaled ? bytes[at] : 0;
+        g.sb_inst = scaled ? bytes[at + 1] : 0;
+        if (instances > 1 && ((g.a_inst | g.b_inst | g.c_inst) & 15))
+            return fail(MS_ERR_BAD_ARG, "ms_variant_launch: several instances of the product need copies of whole 16 bytes");
+        g.rows = (int32_t)op.M;
+        g.cols = (int32_t)op.N;
+        g.depth = (int32_t)op.K;
+        g.experts = (int32_t)op.nb;
+        args[0] = &g;
+    }
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    const int32_t rc = load_layer(v, dev);
+    if (rc != MS_OK) return rc;
+    HIP_TRY(hipModuleLaunchKernel(v->fn, gx, gy, 1, v->spec.block[0], 1, 1, 0, (hipStream_t)stream, args, nullptr));
     return MS_OK;
 }
 
@@ -356,7 +478,7 @@ extern "C" int32_t ms_variant_launch_static(ms_variant *v, const void *const *in
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
     ms_variant *run = v;
-    if (inputs[0] && (v->p.family == MS_FAM_REDUCE || inputs[1])) (void)runs(v, inputs, instances, false, &run);
+    if (!is_layer_family(v->p.family) && inputs[0] && (v->p.family == MS_FAM_REDUCE || inputs[1])) (void)runs(v, inputs, instances, false, &run);
     if (v->device != dev || !v->fn || !run || run->device != dev || !run->fn)
         return fail(MS_ERR_BAD_ARG, "ms_variant_launch_static: call ms_variant_prepare on device %d first (loading a kernel allocates)", dev);
     const size_t need = workspace_per_instance(v) * (size_t)instances;
@@ -377,6 +499,7 @@ extern "C" int32_t ms_variant_launch(ms_variant *v, const void *const *inputs, v
 {
     if (!v || !inputs || !outputs) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: NULL argument");
     if (instances < 1) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: instances = %d", instances);
+    if (is_layer_family(v->p.family)) return launch_layer(v, inputs, outputs, instances, stream);
     if (v->p.rfactor > 1 && !workspace)
         return fail(MS_ERR_BAD_ARG, "ms_variant_launch: the variant splits its reduction over %d workgroups and needs a workspace of %zu bytes per instance",
                     v->p.rfactor, workspace_per_instance(v));
@@ -504,6 +627,22 @@ extern "C" int32_t ms_measure(ms_variant *v, const ms_bufset *sets, int32_t n_se
     auto launch = [&]() -> int32_t {
         const ms_bufset &b = sets[set];
         set = (set + 1) % n_sets;
+        if (is_layer_family(v->p.family)) {
+            // one block for the outputs, one for the inputs from the fourth on where there are five
+            auto next = [&](const void *p, int idx) -> char * {
+                int64_t bytes = 0;
+                (void)ms_op_tensor_bytes(&v->op, idx, &bytes);
+                return p ? (char *)p + (bytes * cfg->instances + 255) / 256 * 256 : nullptr;
+            };
+            void *outs[3] = {b.output, nullptr, nullptr};
+            if (v->op.d.kind == MS_OP_RMS_NORM) {
+                outs[1] = next(outs[0], -1);
+                outs[2] = next(outs[1], -2);
+            }
+            const void *ins[5] = {b.inputs[0], b.inputs[1], b.inputs[2], b.inputs[3], nullptr};
+            if (layer_inputs(v->op) == 5) ins[4] = next(ins[3], 3);
+            return ms_variant_launch(v, ins, outs, b.workspace, cfg->instances, stream);
+        }
         void *outs[1] = {b.output};
         return ms_variant_launch(v, b.inputs, outs, b.workspace, cfg->instances, stream);
     };
