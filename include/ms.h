@@ -458,12 +458,13 @@ typedef enum ms_body {
                                 into LDS; body_tile = 32-pixel tiles of a wavefront */
     MS_BODY_RMS_ROWS = 10,   /* RMS_NORM: rows in the registers of a workgroup; body_tile = wavefronts that share a row */
     MS_BODY_RAGGED_TILES = 11, /* products over rows by expert: tiles whose operands lie in LDS; body_tile = 1000 * rows + columns */
+    MS_BODY_RAGGED_PHASES = 13, /* the same in tiles of 256 x 256 under persistent workgroups whose wavefronts read and multiply in turn */
     MS_BODY_RAGGED_ROWS = 12,  /* the same of few rows for each expert: wavefronts of a workgroup share its reduction */
     MS_BODY_FEW_ROWS = 9     /* the same of a nest over up to 128 rows times a row-major matrix (fp16, bf16), of launches of up to 64 x 64
                                 outputs per compute unit: wavefronts of a workgroup share its reduction; body_tile packs the tile */
 } ms_body;
 
-/* Bodies 10 to 12 are those of the layers of language models, whose kernels take sizes as arguments. */
+/* Bodies 10 to 13 are those of the layers of language models, whose kernels take sizes as arguments. */
 
 /* What the trace interpreter derives.  Unused fields are zero.  With bodies 1 to 3 and 6, block_*, grid, threads,
  * waves, acc_per_thread, lds_bytes, vec and vec_b are those of the kernel that runs, and so are the splits ti, tj, tc and tk

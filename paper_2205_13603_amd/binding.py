@@ -27,8 +27,9 @@ SPACE_DEFAULT = 0xFF
 STATIC_WORKSPACE_BYTES = 32 << 20
 FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE, FAM_RMS_NORM, FAM_RAGGED = range(6)
 (BODY_NEST, BODY_ROW_VECTORS, BODY_STRIPS, BODY_IMAGE_ROWS, BODY_PHASES, BODY_DOUBLE_STEPS, BODY_CONV_STEPS, BODY_CONV_PATCH, BODY_CONV_PLANES,
- BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS) = range(13)
+ BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS, BODY_RAGGED_PHASES) = range(14)
 EPS_UNIT, MAX_EXPERTS, SCALE_BLOCK = 1e-12, 1024, 128
+LAYERS = (OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD)
 MAX_SLOTS, MAX_FACTORS, MAX_CANDS, MAX_LOOPS = 16, 4, 12, 8
 
 F8E4M3 = 5
@@ -216,11 +217,12 @@ SYMBOLS = {
 
 _lib = None
 _launch_native = None  # launch(variant address, inputs, output, instances, stream, workspace) -> status
+_launch_layer = None   # the same of operators with more inputs and outputs
 
 
 def lib():
     """Load libms.so (built by build_lib.py / __graft_entry__.build()).  Raises if it is missing."""
-    global _lib, _launch_native
+    global _lib, _launch_native, _launch_layer
     if _lib is None:
         if not os.path.exists(LIB_PATH):
             raise OSError("%s is missing: run `python -m paper_2205_13603_amd.build_lib` (there is no fallback path)" % LIB_PATH)
@@ -241,6 +243,7 @@ def lib():
             raise OSError("_launch.so is missing: run `python -m paper_2205_13603_amd.build_lib` (there is no fallback path): %s" % e)
         _launch.bind(C.cast(L.ms_variant_launch, C.c_void_p).value)
         _launch_native = _launch.launch
+        _launch_layer = _launch.launch_layer
         _lib = L
     return _lib
 
@@ -269,6 +272,7 @@ class Op:
             d.a_strides[i] = v
         for i, v in enumerate(b_strides or ()):
             d.b_strides[i] = v
+        self.kind = kind
         self.handle = C.c_void_p()
         _check(lib().ms_op_create(C.byref(d), C.byref(self.handle)))
 
@@ -574,6 +578,7 @@ class Variant:
         self.handle = C.c_void_p()
         _check(lib().ms_variant_build(op.handle, C.byref(space), C.byref(trace), C.byref(self.handle)))
         self._address = self.handle.value
+        self._launch = _launch_layer if op.kind in LAYERS else _launch_native
 
     def __del__(self):
         if getattr(self, "handle", None) and _lib is not None:
@@ -613,7 +618,7 @@ class Variant:
 
     def launch(self, inputs, output, instances=1, stream=None, workspace=None):
         """inputs / output / workspace: device pointers (ints); output: a sequence of them for an operator of several outputs."""
-        rc = _launch_native(self._address, inputs, output, instances, stream, workspace)
+        rc = self._launch(self._address, inputs, output, instances, stream, workspace)
         if rc:
             _check(rc)
 

@@ -33,7 +33,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             int *table = reinterpret_cast<int *>(lds + TABLE_AT);
             if (wave == 0) count_tiles(offsets, g.experts, g.rows, BM, lane, table);
             barrier();
-            const unsigned total = (unsigned)table[g.experts - 1] * nt;
+            const unsigned total = uniform((unsigned)table[g.experts - 1]) * nt;
             if (blockIdx.x >= total) return;
             const unsigned f = xcd_run<0>(blockIdx.x, total);
             where = find_tile(table, g.experts, f / nt, lane);
@@ -41,8 +41,8 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             of = f - (unsigned)(f / nt - where.tile) * nt;
             const range_t r = rows_of(offsets, where.expert, g.rows);
             expert = where.expert;
-            first = r.first;
-            end = r.last;
+            first = __builtin_amdgcn_readfirstlane(r.first);
+            end = __builtin_amdgcn_readfirstlane(r.last);
         } else {
             of = xcd_run<0>(blockIdx.x, (unsigned)where.tiles * nt);
         }
@@ -56,11 +56,11 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 
     // ---- 8 rows of 128 bytes per load instruction, 16-byte chunks swizzled by the row so that a fragment read meets each bank once
     unsigned avoff[LA], bvoff[LB];
-    auto chunk = [&](int l) { return lane % 8 ^ (l % 2 * 4 + lane / 16); };
+    const int chunk = lane % 8 ^ lane / 8;
 #pragma unroll
-    for (int l = 0; l < LA; ++l) avoff[l] = l * 8 + lane / 8 < rows ? (unsigned)((l * 8 + lane / 8) * (int)g.a_row + chunk(l) * 16) : OUTSIDE;
+    for (int l = 0; l < LA; ++l) avoff[l] = l * 8 + lane / 8 < rows ? (unsigned)((l * 8 + lane / 8) * (int)g.a_row + chunk * 16) : OUTSIDE;
 #pragma unroll
-    for (int l = 0; l < LB; ++l) bvoff[l] = l * 8 + lane / 8 < cols ? (unsigned)((l * 8 + lane / 8) * (int)g.b_row + chunk(l) * 16) : OUTSIDE;
+    for (int l = 0; l < LB; ++l) bvoff[l] = l * 8 + lane / 8 < cols ? (unsigned)((l * 8 + lane / 8) * (int)g.b_row + chunk * 16) : OUTSIDE;
     const int bytes = g.depth * ES, blocks = (bytes + 127) / 128;
     const int mine = blocks > wave ? (blocks - wave + NW - 1) / NW : 0; // blocks of this wavefront
     const unsigned ring = lds_address(lds) + wave * STAGES * SLOT;
@@ -75,9 +75,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         const unsigned at = ring + stage * SLOT;
         const bool tail = here < 128;
 #pragma unroll
-        for (int l = 0; l < LB; ++l) gather_lds16_at(rb, tail && chunk(l) * 16 >= here ? OUTSIDE : bvoff[l], 0, at + BM * 128 + l * 1024);
+        for (int l = 0; l < LB; ++l) gather_lds16_at(rb, tail && chunk * 16 >= here ? OUTSIDE : bvoff[l], 0, at + BM * 128 + l * 1024);
 #pragma unroll
-        for (int l = 0; l < LA; ++l) gather_lds16_at(ra, tail && chunk(l) * 16 >= here ? OUTSIDE : avoff[l], 0, at + l * 1024);
+        for (int l = 0; l < LA; ++l) gather_lds16_at(ra, tail && chunk * 16 >= here ? OUTSIDE : avoff[l], 0, at + l * 1024);
 #if IN_DT == DT_F8E4M3
         gather_lds4(sa, lane < rows ? (unsigned)(lane * blocks + k) * 4 : OUTSIDE, at + (BM + BN) * 128);
         gather_lds4(sb, lane == 0 ? (unsigned)k * 4 : OUTSIDE, at + (BM + BN) * 128 + 256);
@@ -106,10 +106,10 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         auto frag = [&](const char *r, int q) {
             frag_t f;
             if (ES == 2) {
-                f.v[0] = *reinterpret_cast<const u4_t *>(r + ((q * 4 + lgrp) ^ lrow >> 1) * 16);
+                f.v[0] = *reinterpret_cast<const u4_t *>(r + ((q * 4 + lgrp) ^ lrow % 8) * 16);
             } else {
 #pragma unroll
-                for (int h = 0; h < (int)(sizeof(frag_t) / 16); ++h) f.v[h] = *reinterpret_cast<const u4_t *>(r + ((lgrp * 2 + h) ^ lrow >> 1) * 16);
+                for (int h = 0; h < (int)(sizeof(frag_t) / 16); ++h) f.v[h] = *reinterpret_cast<const u4_t *>(r + ((h * 4 + lgrp) ^ lrow % 8) * 16);
             }
             return f;
         };

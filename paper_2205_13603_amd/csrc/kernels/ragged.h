@@ -20,7 +20,8 @@ typedef int i8v_t __attribute__((ext_vector_type(8)));
 // One matrix-core step.  The operands are swapped, so that a lane holds four consecutive columns of one row: rows lane % 16, columns
 // 4 * (lane / 16) and on.
 #if IN_DT == DT_F8E4M3
-struct frag_t { u4_t v[2]; }; // 32 k values
+struct frag_t { u4_t v[2]; }; // 32 k values: chunks lane / 16 and 4 + lane / 16 of a row's 128 bytes, for both operands alike (chunks 2 lane / 16
+                              // and on would meet the banks of other rows: 42 % of the LDS cycles of 8192^3)
 __device__ __forceinline__ f4_t mfma(const frag_t &b, const frag_t &a, f4_t c)
 {
     // format selectors 0 = this 8-bit float for both operands; zero scale operands select the unscaled form
@@ -80,14 +81,44 @@ __device__ __forceinline__ void count_tiles(const int *offsets, int experts, int
     }
 }
 
+// The same of tiles of 256 rows, with the rest of an expert's rows a tile only where it is more than half of one; `halves`: experts up
+// to and including e whose rest is less.
+__device__ __forceinline__ void count_wide_tiles(const int *offsets, int experts, int total, int lane, int *table, unsigned short *halves)
+{
+    int before = 0, before_h = 0;
+    for (int e0 = 0; e0 < experts; e0 += 64) {
+        const int e = e0 + lane;
+        int n = 0, h = 0;
+        if (e < experts) {
+            const range_t r = rows_of(offsets, e, total);
+            n = (r.last - r.first + 127) / 256;
+            h = r.last - r.first > n * 256;
+        }
+        const unsigned long m = __ballot(h); // halves of the lanes up to this one
+        h = before_h + __builtin_popcountl(m & (~0ul >> (63 - lane)));
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) {
+            const int x = __builtin_amdgcn_ds_bpermute((lane - d) * 4, n);
+            n += lane >= d ? x : 0;
+        }
+        n += before;
+        if (e < experts) {
+            table[e] = n;
+            halves[e] = (unsigned short)h;
+        }
+        before = __builtin_amdgcn_readlane(n, 63);
+        before_h += __builtin_popcountl(m);
+    }
+}
+
 // Expert of row tile `t`, and which of the expert's tiles it is; all lanes of a wavefront together.
 struct tile_at { int expert, tile, tiles; };
-__device__ __forceinline__ tile_at find_tile(const int *table, int experts, int t, int lane)
+template <class T> __device__ __forceinline__ tile_at find_tile(const T *table, int experts, int t, int lane)
 {
     int e0 = 0;
     for (;; e0 += 64) {
         const int e = e0 + lane;
-        const bool behind = e < experts ? table[e] > t : true;
+        const bool behind = e < experts ? (int)table[e] > t : true;
         const unsigned long m = __ballot(behind);
         if (m) {
             int e1 = e0 + __builtin_ctzl(m);
@@ -97,6 +128,73 @@ __device__ __forceinline__ tile_at find_tile(const int *table, int experts, int 
         }
     }
 }
+
+#ifdef WGRAD // tiles of rows and columns
+struct tile_t {
+    int expert, row, rows, col; // first row (of A and C; WGRAD: of D[e]) and how many rows the tile has, first column
+    int k0, depth;              // first row and number of rows of the reduction
+};
+
+// The launch's tiles; `table` as count_tiles filled it.
+template <int TR, int TC> __device__ __forceinline__ unsigned tiles_of(const ragged_args &g, const int *table)
+{
+    const unsigned nt = (unsigned)(g.cols + TC - 1) / TC;
+    if (GROUPED && !WGRAD) return uniform((unsigned)table[g.experts - 1]) * nt;
+    return (unsigned)((g.rows + TR - 1) / TR) * nt * (WGRAD ? (unsigned)g.experts : 1u);
+}
+
+// Tile `f`; false: there is nothing to do (offsets that decrease: nothing outside the tensors is touched).  Of an expert 8 row tiles by all
+// columns at a time, rows first.  WIDE: row tiles as count_wide_tiles counts them.  `order` (WGRAD): the experts in the order in which their
+// tiles are made.
+template <int TR, int TC, bool WIDE = false> __device__ __forceinline__ bool decode(const ragged_args &g, const int *offsets, const int *table, unsigned f, int lane, tile_t &t, const unsigned short *order = nullptr)
+{
+    const unsigned nt = (unsigned)(g.cols + TC - 1) / TC;
+    tile_at where;
+    unsigned of;
+    if (WGRAD || !GROUPED) {
+        const int mt = WIDE ? (g.rows + 127) / 256 : (g.rows + TR - 1) / TR;
+        const unsigned each = (unsigned)mt * nt;
+        where = {(int)(f / each), 0, mt};
+        of = f % each;
+        if (WGRAD && each % 8 == 0) of = xcd_run<0>(of, each); // an expert's tiles over all XCDs: experts differ in their rows
+        if (order) where.expert = order[where.expert];
+    } else {
+        where = find_tile(table, g.experts, (int)(f / nt), lane);
+        if ((unsigned)where.tile >= (unsigned)where.tiles) return false;
+        of = f - (f / nt - (unsigned)where.tile) * nt;
+    }
+    constexpr unsigned GM = 8;
+    const unsigned band = of / (GM * nt), in = of - band * GM * nt, rest = (unsigned)where.tiles - band * GM, high = rest < GM ? rest : GM;
+    t.expert = where.expert;
+    t.col = (int)(in / high) * TC;
+    t.row = (int)(band * GM + in % high) * TR;
+    t.k0 = 0;
+    t.depth = g.depth;
+    int end = g.rows;
+    if (GROUPED) {
+        const range_t r = rows_of(offsets, t.expert, WGRAD ? g.depth : g.rows);
+        const int first = __builtin_amdgcn_readfirstlane(r.first), last = __builtin_amdgcn_readfirstlane(r.last);
+        if (WGRAD) {
+            t.k0 = first;
+            t.depth = last - first;
+        } else {
+            t.row += first;
+            end = last;
+        }
+    }
+    t.rows = end - t.row < TR ? end - t.row : TR;
+    // divisions are made on the vector unit; the tile is the same in all lanes, and its fields belong in scalar registers
+    t = {__builtin_amdgcn_readfirstlane(t.expert), __builtin_amdgcn_readfirstlane(t.row), __builtin_amdgcn_readfirstlane(t.rows), __builtin_amdgcn_readfirstlane(t.col), t.k0, t.depth};
+    return t.rows > 0;
+}
+
+// Tile `f` of `total` in the order of launch: products deal runs of tiles to the XCDs, so that the workgroups that run together on one XCD
+// share rows and columns in its L2.
+template <int TR, int TC> __device__ __forceinline__ bool find(const ragged_args &g, const int *offsets, const int *table, unsigned f, unsigned total, int lane, tile_t &t)
+{
+    return decode<TR, TC>(g, offsets, table, WGRAD ? f : xcd_run<0>(f, total), lane, t);
+}
+#endif
 
 // 4 bytes per lane from a buffer to `dst` (wave-uniform) + 4 * lane; as gather_lds16 in common.h
 __device__ __forceinline__ void gather_lds4(const rsrc_t &buffer, unsigned voff, unsigned dst)

@@ -1,0 +1,276 @@
+// One tile of a product over rows by expert, or of the gradient of the experts' matrices, by all wavefronts of a workgroup: TR rows by TC columns,
+// WR by WC wavefronts, ring of STAGES.
+//
+// k steps of 128 bytes of each row of the operands go straight into a ring of LDS stages; operands contiguous along k (A_KC, B_KC)
+// lie there as rows of eight 16-byte chunks, swizzled by the row so that a fragment read meets each bank once; the others as rows of
+// k, in 32-byte granules swizzled by k, read with the transposing LDS loads.  What lies behind an expert's rows, the last column or the last
+// k is read as zeros and not stored.
+template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
+    static constexpr int BM = TR, BN = TC, WI = WR, WJ = WC, STAGES = RING, NW = WI * WJ, TM = BM / WI / 16, TN = BN / WJ / 16, BK = 128 / ES;
+    static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
+    static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB; // load instructions of a wavefront and step
+    static constexpr bool SCALED = IN_DT == DT_F8E4M3;
+    static constexpr int KB = 8;                                              // k blocks whose scales are in LDS at a time, twice
+    static constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, SB_BYTES = SCALED ? 256 : 0;
+    static constexpr int SC_AT = STAGES * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LDS_BYTES = SB_AT + 2 * SB_BYTES;
+    static constexpr int LS = SCALED ? KB * BM / 64 / NW : 0;                 // load instructions of a wavefront for the scales of KB blocks
+    static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wavefront issues the same loads");
+    static_assert(BM >= 64 && 128 % (TN * 16) == 0, "a wavefront's columns share a scale");
+
+    // `lds`: LDS_BYTES that no wavefront uses any more
+    static __device__ __forceinline__ void make(const ragged_args &g, int inst, const tile_t &t, char *lds)
+    {
+        const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+        const int wi = wave / WJ, wj = wave % WJ, lrow = lane % 16, lgrp = lane / 16;
+        const int cols = g.cols - t.col < BN ? g.cols - t.col : BN;
+        const int steps = (t.depth + BK - 1) / BK;
+
+        // ---- operands: of each load instruction the lane's place from the tile's first element, OUTSIDE where there is nothing
+        const char *a = g.a + inst * g.a_inst + (A_KC ? (long)t.row * g.a_row : (long)t.k0 * g.a_row + (long)t.row * ES);
+        const char *b = g.b + inst * g.b_inst + t.expert * g.b_expert + (B_KC ? (long)t.col * g.b_row : (long)t.k0 * g.b_row + (long)t.col * ES);
+        // chunk of 16 bytes of a k-contiguous row, the same in all of a wavefront's instructions
+        const int chunk = lane % 8 ^ lane / 8;
+        // k row and first column of a transposed operand
+        auto tr_k = [&](int width, int l) { return (wave + l * NW) * (512 / width) + lane * 8 / width; };
+        auto tr_col = [&](int width, int l) {
+            const int k = tr_k(width, l), slot = lane * 8 % width / 8, swz = (k & 3 | k >> 1 & 4) & (width / 16 - 1);
+            return ((slot >> 1 ^ swz) << 4) + (slot & 1) * 8;
+        };
+        unsigned avoff[LA], bvoff[LB];
+#pragma unroll
+        for (int l = 0; l < LA; ++l) {
+            if (A_KC) {
+                const int r = (wave + l * NW) * 8 + lane / 8;
+                avoff[l] = r < t.rows ? (unsigned)(r * (int)g.a_row + chunk * 16) : OUTSIDE;
+            } else {
+                const int c = tr_col(BM, l);
+                avoff[l] = c < t.rows ? (unsigned)(tr_k(BM, l) * (int)g.a_row + c * ES) : OUTSIDE;
+            }
+        }
+#pragma unroll
+        for (int l = 0; l < LB; ++l) {
+            if (B_KC) {
+                const int r = (wave + l * NW) * 8 + lane / 8;
+                bvoff[l] = r < cols ? (unsigned)(r * (int)g.b_row + chunk * 16) : OUTSIDE;
+            } else {
+                const int c = tr_col(BN, l);
+                bvoff[l] = c < cols ? (unsigned)(tr_k(BN, l) * (int)g.b_row + c * ES) : OUTSIDE;
+            }
+        }
+        const unsigned lds0 = lds_address(lds);
+#if ALIGNED
+        auto load = [&](int step, int stage) {
+            const bool tail = step * BK + BK > t.depth; // elements of k that there are not
+            const int here = t.depth - step * BK;
+            const rsrc_t ra = buffer_at(a + (A_KC ? (long)step * 128 : (long)step * BK * g.a_row)), rb = buffer_at(b + (B_KC ? (long)step * 128 : (long)step * BK * g.b_row));
+            const unsigned at = lds0 + stage * STAGE + wave * 1024;
+#pragma unroll
+            for (int l = 0; l < LA; ++l) {
+                unsigned v = avoff[l];
+                if (tail) v = (A_KC ? chunk * (16 / ES) : tr_k(BM, l)) < here ? v : OUTSIDE;
+                gather_lds16_at(ra, v, 0, at + l * NW * 1024);
+            }
+#pragma unroll
+            for (int l = 0; l < LB; ++l) {
+                unsigned v = bvoff[l];
+                if (tail) v = (B_KC ? chunk * (16 / ES) : tr_k(BN, l)) < here ? v : OUTSIDE;
+                gather_lds16_at(rb, v, 0, at + A_BYTES + l * NW * 1024);
+            }
+        };
+#else
+        // Rows that start anywhere, extents that are no whole 16 bytes: element by element through registers.
+        auto load = [&](int step, int stage) {
+            auto one = [&](const char *p, bool kc, unsigned voff, int k, int c, int high, int at) {
+                union { in_t e[16 / ES]; u4_t v; } x;
+#pragma unroll
+                for (int i = 0; i < 16 / ES; ++i) {
+                    const bool there = voff != OUTSIDE && (kc ? k + i < t.depth : k < t.depth && c + i < high);
+                    x.e[i] = in_t(0);
+                    if (there) x.e[i] = reinterpret_cast<const in_t *>(p + voff)[i];
+                }
+                *reinterpret_cast<u4_t *>(lds + at + lane * 16) = x.v;
+            };
+            const char *pa = a + (A_KC ? (long)step * 128 : (long)step * BK * g.a_row), *pb = b + (B_KC ? (long)step * 128 : (long)step * BK * g.b_row);
+#pragma unroll 1
+            for (int l = 0; l < LA; ++l) {
+                const int r = (wave + l * NW) * 8 + lane / 8, c = tr_col(BM, l);
+                const unsigned v = A_KC ? (r < t.rows ? (unsigned)(r * (int)g.a_row + chunk * 16) : OUTSIDE) : (c < t.rows ? (unsigned)(tr_k(BM, l) * (int)g.a_row + c * ES) : OUTSIDE);
+                one(pa, A_KC, v, step * BK + (A_KC ? chunk * (16 / ES) : tr_k(BM, l)), c, t.rows, stage * STAGE + (wave + l * NW) * 1024);
+            }
+#pragma unroll 1
+            for (int l = 0; l < LB; ++l) {
+                const int r = (wave + l * NW) * 8 + lane / 8, c = tr_col(BN, l);
+                const unsigned v = B_KC ? (r < cols ? (unsigned)(r * (int)g.b_row + chunk * 16) : OUTSIDE) : (c < cols ? (unsigned)(tr_k(BN, l) * (int)g.b_row + c * ES) : OUTSIDE);
+                one(pb, B_KC, v, step * BK + (B_KC ? chunk * (16 / ES) : tr_k(BN, l)), c, cols, stage * STAGE + A_BYTES + (wave + l * NW) * 1024);
+            }
+        };
+#endif
+
+        // ---- scales of KB blocks: [block][row], gathered from rows of blocks; those of the columns beside them
+#if IN_DT == DT_F8E4M3
+        const int blocks = (g.depth + 127) / 128, col_blocks = (g.cols + 127) / 128;
+        const char *sa = (const char *)g.sa + inst * g.sa_inst + (long)t.row * blocks * 4;
+        const char *sb = (const char *)g.sb + inst * g.sb_inst + ((long)t.expert * col_blocks + t.col / 128) * blocks * 4;
+        auto load_scales = [&](int first) {
+            const rsrc_t r = buffer_at(sa + first * 4);
+            const unsigned at = lds0 + SC_AT + first / KB % 2 * SC_BYTES;
+#pragma unroll
+            for (int l = 0; l < LS; ++l) {
+                const int i = wave * LS + l, row = i / KB * 64 + lane, k = i % KB; // the blocks of one line follow each other
+                gather_lds4(r, row < t.rows && first + k < blocks ? (unsigned)(row * blocks + k) * 4 : OUTSIDE, at + (k * BM + i / KB * 64) * 4);
+            }
+            if (wave == 0) { // columns: lane = 8 * (block of columns) + block of k
+                const int n = lane / KB;
+                gather_lds4(buffer_at(sb + first * 4), n < (BN + 127) / 128 && t.col / 128 + n < col_blocks && first + lane % KB < blocks ? (unsigned)(n * blocks + lane % KB) * 4 : OUTSIDE,
+                            lds0 + SB_AT + first / KB % 2 * SB_BYTES);
+            }
+        };
+#endif
+
+        f4_t acc[TM][TN];
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+
+        // ---- fragments
+        // of 16 rows from `row0` of a k-contiguous operand at `p`, matrix-core step q
+        auto frag_kc = [&](const char *p, int row0, int q) {
+            frag_t f;
+            const char *r = p + row0 * 128 + lrow * 128;
+            if (ES == 2) {
+                f.v[0] = *reinterpret_cast<const u4_t *>(r + ((q * 4 + lgrp) ^ lrow % 8) * 16);
+            } else {
+#pragma unroll
+                for (int h = 0; h < (int)(sizeof(frag_t) / 16); ++h) f.v[h] = *reinterpret_cast<const u4_t *>(r + ((h * 4 + lgrp) ^ lrow % 8) * 16);
+            }
+            return f;
+        };
+        // of 16 columns from `col0` of a transposed operand of `width` columns
+        auto frag_tr = [&](const char *p, int width, int col0, int q) {
+            frag_t f;
+#if IN_DT != DT_F8E4M3
+            typedef short tr4_t __attribute__((ext_vector_type(4)));
+            struct { tr4_t v[2]; } x;
+            const int r = lrow / 4, swz = (r | (lgrp & 1) << 2) & (width / 16 - 1);
+            const char *at = p + (q * 32 + lgrp * 8 + r) * width * 2 + ((col0 / 16) ^ swz) * 32 + lrow % 4 * 8;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+                x.v[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) tr4_t *)(at + h * 4 * width * 2));
+            f.v[0] = __builtin_bit_cast(u4_t, x);
+#endif
+            return f;
+        };
+        auto frag_a = [&](int stage, int tm, int q) {
+            const char *p = lds + stage * STAGE;
+            return A_KC ? frag_kc(p, (wi * TM + tm) * 16, q) : frag_tr(p, BM, (wi * TM + tm) * 16, q);
+        };
+        auto frag_b = [&](int stage, int tn, int q) {
+            const char *p = lds + stage * STAGE + A_BYTES;
+            return B_KC ? frag_kc(p, (wj * TN + tn) * 16, q) : frag_tr(p, BN, (wj * TN + tn) * 16, q);
+        };
+
+        // ---- the ring
+#if IN_DT == DT_F8E4M3
+        if (steps) load_scales(0);
+#endif
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s)
+            if (s < steps) load(s, s);
+        int stage = 0;
+#pragma unroll 1
+        for (int s = 0; s < steps; ++s) {
+            // this step's loads have landed; those of the steps behind it may be in flight (the few loads of scales among them only
+            // make a wait longer)
+            if (STAGES > 2 && s + STAGES - 2 < steps) DL_WAIT_VM((STAGES - 2) * LOADS);
+            else DL_WAIT_VM(0);
+            barrier();
+#if IN_DT == DT_F8E4M3
+            if (s % KB == 0) load_scales(s + KB); // beyond the last block: zeros
+#endif
+            if (s + STAGES - 1 < steps) load(s + STAGES - 1, stage ? stage - 1 : STAGES - 1);
+            frag_t fa[KQ][TM], fb[KQ][TN];
+#pragma unroll
+            for (int q = 0; q < KQ; ++q) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) fb[q][j] = frag_b(stage, j, q);
+#pragma unroll
+                for (int i = 0; i < TM; ++i) fa[q][i] = frag_a(stage, i, q);
+            }
+#if IN_DT == DT_F8E4M3
+            const float *sc = reinterpret_cast<const float *>(lds + SC_AT + s / KB % 2 * SC_BYTES) + s % KB * BM + wi * TM * 16 + lrow;
+            const float sj = reinterpret_cast<const float *>(lds + SB_AT + s / KB % 2 * SB_BYTES)[(t.col % 128 + wj * TN * 16) / 128 * KB + s % KB];
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const float f = sc[i * 16] * sj;
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const f4_t d = mfma(fb[0][j], fa[0][i], f4_t{0, 0, 0, 0});
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], f, acc[i][j][v]);
+                }
+            }
+#else
+#pragma unroll
+            for (int q = 0; q < KQ; ++q)
+#pragma unroll
+                for (int i = 0; i < TM; ++i)
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fb[q][j], fa[q][i], acc[i][j]);
+#endif
+            stage = stage + 1 == STAGES ? 0 : stage + 1;
+        }
+
+        // ---- results
+        constexpr int OS = sizeof(out_t);
+        char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
+        if constexpr (OS == 4) {
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+                const int r = (wi * TM + i) * 16 + lrow;
+                if (r < t.rows) {
+#pragma unroll
+                    for (int j = 0; j < TN; ++j) {
+                        const int col = (wj * TN + j) * 16 + lgrp * 4;
+                        if (col < cols) store4(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, acc[i][j], cols - col);
+                    }
+                }
+            }
+        } else {
+            // 16 rows at a time by way of LDS, so that a row's columns leave as whole lines
+            constexpr int CH = TN * 2; // 16-byte chunks of a wavefront's row
+            barrier();                 // the last step's operands have been read
+            char *const mine = lds + wave * (16 * CH * 16);
+            static_assert(NW * 16 * CH * 16 <= STAGES * STAGE, "results fit where the operands were");
+#pragma unroll
+            for (int i = 0; i < TM; ++i) {
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    struct { out_t v[4]; } o;
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o.v[v] = from_acc(acc[i][j][v]);
+                    *reinterpret_cast<decltype(o) *>(mine + (lrow * CH + ((j * 2 + lgrp / 2) ^ (lrow % CH))) * 16 + lgrp % 2 * 8) = o;
+                }
+                lds_done();
+#pragma unroll
+                for (int l = 0; l < 16 * CH / 64; ++l) {
+                    const int r = (l * 64 + lane) / CH, ch = lane % CH;
+                    struct __attribute__((aligned(16))) { out_t v[8]; } o = *reinterpret_cast<const decltype(o) *>(mine + (r * CH + (ch ^ r % CH)) * 16);
+                    const int row = (wi * TM + i) * 16 + r, col = wj * TN * 16 + ch * 8;
+                    if (row < t.rows && col < cols) {
+                        char *dst = c + ((long)(t.row + row) * g.cols + t.col + col) * OS;
+                        if (col + 8 <= cols) {
+                            struct __attribute__((packed, aligned(2))) any_t { out_t v[8]; };
+                            *reinterpret_cast<any_t *>(dst) = __builtin_bit_cast(any_t, o);
+                        } else {
+#pragma unroll
+                            for (int v = 0; v < 8; ++v)
+                                if (col + v < cols) reinterpret_cast<out_t *>(dst)[v] = o.v[v];
+                        }
+                    }
+                }
+                lds_done();
+            }
+        }
+    }
+};

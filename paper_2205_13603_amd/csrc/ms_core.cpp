@@ -1207,7 +1207,7 @@ extern "C" int32_t ms_trace_to_text(const ms_op *op, const ms_space *space, cons
         if (is_layer_family(p.family)) {
             if (p.body == MS_BODY_RMS_ROWS) appendf(s, "# body=rms-rows: %d wavefronts share a row, which stays in their registers\n", p.body_tile);
             else appendf(s, "# body=%s: %d rows of one expert x %d columns per workgroup, the last of each masked\n",
-                         p.body == MS_BODY_RAGGED_ROWS ? "ragged-rows" : "ragged-tiles", p.block_m, p.block_n);
+                         p.body == MS_BODY_RAGGED_ROWS ? "ragged-rows" : p.body == MS_BODY_RAGGED_PHASES ? "ragged-phases" : "ragged-tiles", p.block_m, p.block_n);
             appendf(s, "# sizes are arguments of the kernel; workgroup=%d threads, grid=%d, lds=%d B\n", p.threads, p.grid[0], p.lds_bytes);
             if (needed) *needed = s.size() + 1;
             if (buf && cap) {

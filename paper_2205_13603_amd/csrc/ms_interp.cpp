@@ -716,6 +716,8 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
         t.wj = code == 256256 ? 4 : 2;
         t.stages = code == 64128 ? 3 : 2;
         t.lds = (int64_t)t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
+        if (code == 256256 && op->out_size == 2) t.lds += 8192; // where results are put together as lines
+        if (code == 256256 && (table || op->d.kind == MS_OP_GROUPED_WGRAD)) t.lds += 2048; // experts without a whole tile; their order
     }
     return t;
 }
@@ -740,7 +742,7 @@ int64_t ragged_rule(const ms_op *op)
         if (rows <= 32) return 32032;
     }
     if (rows <= 64) return 64128;
-    return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 && rows >= 192 ? 256256 : 128128;
+    return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 && rows >= 192 && layer_block_fits(op, 256256) ? 256256 : 128128;
 }
 
 int64_t rms_rule(const ms_op *op)
@@ -778,7 +780,7 @@ int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *tr
         const bool aligned = ragged_aligned(op);
         if (!code) code = ragged_rule(op);
         const RaggedTile t = ragged_tile(op, code);
-        p->body = t.few ? MS_BODY_RAGGED_ROWS : MS_BODY_RAGGED_TILES;
+        p->body = t.few ? MS_BODY_RAGGED_ROWS : code == 256256 ? MS_BODY_RAGGED_PHASES : MS_BODY_RAGGED_TILES;
         p->block_m = t.bm;
         p->block_n = t.bn;
         p->block_k = 128 / op->in_size;
@@ -1451,7 +1453,8 @@ bool ms::layer_block_fits(const ms_op *op, int64_t code)
     const bool few = code % 1000 <= 32;
     if (!ragged_aligned(op)) return code == 64128;
     if (few) return ragged_by_k(op) && (code == 16016 || code == 16032 || code == 32032 || code == 64032);
-    return code == 64128 || code == 128128 || code == 256256;
+    if (code == 256256) return op->in_size == 2 || op->K > 128; // scales of a tile's blocks are overwritten two steps later
+    return code == 64128 || code == 128128;
 }
 
 namespace ms {
@@ -1516,19 +1519,27 @@ int32_t make_kernel_spec(const ms_op *op, const ms_variant_params *p, KernelSpec
         const RaggedTile t = ragged_tile(op, p->body_tile);
         const bool wgrad = d.kind == MS_OP_GROUPED_WGRAD;
         D.push_back(def("GROUPED", d.kind != MS_OP_SCALED_GEMM));
-        D.push_back(def("BM", t.bm));
-        D.push_back(def("BN", t.bn));
-        D.push_back(def("WI", t.wi));
-        D.push_back(def("STAGES", t.stages));
         D.push_back(def("LDS_HOST", t.lds));
         if (!t.few) {
             D.push_back(def("WGRAD", wgrad));
             D.push_back(def("A_KC", !wgrad));
             D.push_back(def("B_KC", ragged_by_k(op)));
-            D.push_back(def("WJ", t.wj));
+        }
+        if (p->body == MS_BODY_RAGGED_ROWS) {
+            D.push_back(def("BM", t.bm));
+            D.push_back(def("BN", t.bn));
+            D.push_back(def("WI", t.wi));
+            D.push_back(def("STAGES", t.stages));
+        }
+        if (p->body == MS_BODY_RAGGED_TILES) {
+            D.push_back(def("TILE_M", t.bm));
+            D.push_back(def("TILE_N", t.bn));
+            D.push_back(def("TILE_WI", t.wi));
+            D.push_back(def("TILE_WJ", t.wj));
+            D.push_back(def("TILE_STAGES", t.stages));
             D.push_back(def("ALIGNED", p->vec > 1));
         }
-        k.template_name = t.few ? "gemm_ragged_rows.hip" : "gemm_ragged.hip";
+        k.template_name = t.few ? "gemm_ragged_rows.hip" : p->body == MS_BODY_RAGGED_PHASES ? "gemm_ragged_phases.hip" : "gemm_ragged.hip";
         *out = k;
         return MS_OK;
     }

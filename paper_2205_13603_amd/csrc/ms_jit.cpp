@@ -108,11 +108,12 @@ static int32_t get_source(const std::string &name, const Source **src) // entrie
     std::string marker = "#include \"common.h\"";
     size_t at = body.find(marker);
     if (at != std::string::npos) body.replace(at, marker.size(), common);
-    marker = "#include \"ragged.h\""; // of the products over rows by expert
-    at = body.find(marker);
-    if (at != std::string::npos) {
+    for (const char *header : {"ragged.h", "ragged_tile.h"}) { // of the products over rows by expert
+        marker = std::string("#include \"") + header + "\"";
+        at = body.find(marker);
+        if (at == std::string::npos) continue;
         std::string shared;
-        if (!read_file(dir + "/ragged.h", &shared)) return fail(MS_ERR_COMPILE, "kernel header %s/ragged.h not found", dir.c_str());
+        if (!read_file(dir + "/" + header, &shared)) return fail(MS_ERR_COMPILE, "kernel header %s/%s not found", dir.c_str(), header);
         body.replace(at, marker.size(), shared);
     }
     const uint64_t hash = hash_bytes(body);

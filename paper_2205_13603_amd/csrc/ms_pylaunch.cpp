@@ -35,11 +35,37 @@ PyObject *bind(PyObject *, PyObject *address)
     Py_RETURN_NONE;
 }
 
-// launch(variant, inputs, output or sequence of outputs, instances, stream, workspace) -> status code
+// launch(variant, inputs, output, instances, stream, workspace) -> status code
 PyObject *launch(PyObject *, PyObject *const *args, Py_ssize_t n)
 {
     if (n != 6 || !g_launch) {
         PyErr_SetString(PyExc_TypeError, "launch(variant, inputs, output, instances, stream, workspace) after bind()");
+        return nullptr;
+    }
+    void *variant, *in[4] = {nullptr, nullptr, nullptr, nullptr}, *out, *stream, *workspace;
+    PyObject *seq = PySequence_Fast(args[1], "inputs: a sequence of device pointers");
+    if (!seq) return nullptr;
+    const Py_ssize_t count = PySequence_Fast_GET_SIZE(seq);
+    bool ok = count <= 4;
+    if (!ok) PyErr_Format(PyExc_ValueError, "%zd inputs, an operator has at most 4", count);
+    for (Py_ssize_t i = 0; ok && i < count; ++i) ok = pointer(PySequence_Fast_GET_ITEM(seq, i), &in[i]);
+    Py_DECREF(seq);
+    if (!ok || !pointer(args[0], &variant) || !pointer(args[2], &out) || !pointer(args[4], &stream) || !pointer(args[5], &workspace)) return nullptr;
+    const int32_t instances = (int32_t)PyLong_AsUnsignedLongMask(args[3]);
+    if (PyErr_Occurred()) return nullptr;
+    int32_t rc;
+    Py_BEGIN_ALLOW_THREADS // the queue of a stream may be full
+    rc = g_launch(variant, in, &out, workspace, instances, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(rc);
+}
+
+// launch_layer(variant, inputs, outputs, instances, stream, workspace): the same of operators with more tensors; outputs is one device
+// pointer or a sequence of them
+PyObject *launch_layer(PyObject *, PyObject *const *args, Py_ssize_t n)
+{
+    if (n != 6 || !g_launch) {
+        PyErr_SetString(PyExc_TypeError, "launch_layer(variant, inputs, outputs, instances, stream, workspace) after bind()");
         return nullptr;
     }
     constexpr Py_ssize_t MOST = 8; // tensors a side
@@ -56,11 +82,13 @@ PyObject *launch(PyObject *, PyObject *const *args, Py_ssize_t n)
     };
     const bool several = PyList_Check(args[2]) || PyTuple_Check(args[2]);
     if (!tensors(args[1], "inputs: a sequence of device pointers", in) ||
-        !(several ? tensors(args[2], "outputs: a sequence of device pointers", out) : pointer(args[2], out)) || !pointer(args[0], &variant) || !pointer(args[4], &stream) || !pointer(args[5], &workspace)) return nullptr;
+        !(several ? tensors(args[2], "outputs: a sequence of device pointers", out) : pointer(args[2], out)) || !pointer(args[0], &variant) ||
+        !pointer(args[4], &stream) || !pointer(args[5], &workspace))
+        return nullptr;
     const int32_t instances = (int32_t)PyLong_AsUnsignedLongMask(args[3]);
     if (PyErr_Occurred()) return nullptr;
     int32_t rc;
-    Py_BEGIN_ALLOW_THREADS // the queue of a stream may be full
+    Py_BEGIN_ALLOW_THREADS
     rc = g_launch(variant, in, out, workspace, instances, stream);
     Py_END_ALLOW_THREADS
     return PyLong_FromLong(rc);
@@ -68,6 +96,7 @@ PyObject *launch(PyObject *, PyObject *const *args, Py_ssize_t n)
 
 PyMethodDef methods[] = {{"bind", bind, METH_O, "address of ms_variant_launch"},
                          {"launch", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(launch)), METH_FASTCALL, "one launch, returns the status code"},
+                         {"launch_layer", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(launch_layer)), METH_FASTCALL, "the same with up to 8 inputs and outputs"},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_launch", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

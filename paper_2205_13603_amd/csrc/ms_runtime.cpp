@@ -387,6 +387,7 @@ static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *cons
     HIP_TRY(hipGetDevice(&dev));
     const int32_t rc = load_layer(v, dev);
     if (rc != MS_OK) return rc;
+    if (v->p.body == MS_BODY_RAGGED_PHASES) gx = (unsigned)std::min<uint64_t>(4ull * gx, (uint64_t)std::max(1, v->compute_units)); // persistent workgroups, of tiles or quarters
     HIP_TRY(hipModuleLaunchKernel(v->fn, gx, gy, 1, v->spec.block[0], 1, 1, 0, (hipStream_t)stream, args, nullptr));
     return MS_OK;
 }

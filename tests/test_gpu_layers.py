@@ -148,7 +148,7 @@ GROUPED = [
 def test_grouped_product(which, kind, out, rows_of_k, code):
     counts, ahead, behind, N, K = GROUPED[which]
     if kind == "f8":
-        K = -(-K // 16) * 16
+        K = max(-(-K // 16) * 16, 144 if code == 256256 else 16)  # tiles of 256 x 256 need two blocks of scales
     E, T = len(counts), ahead + sum(counts) + behind
     if code == -1:  # another small tile each time
         code = [16016, 16032, 32032, 64032, 64128][which % 5] if rows_of_k else 64128
@@ -214,6 +214,43 @@ def test_grouped_product_with_many_experts():
     v = variant(B.grouped_gemm_op(E, sum(counts) + 4, 16, 32, True, "f16"))
     if v is not None:
         check_grouped(v, counts, 2, 2, 16, 32, "f16", "f16", True)
+
+
+@pytest.mark.parametrize("kind,rows_of_k,K", [("bf16", True, 40), ("bf16", True, 72), ("f16", True, 192), ("f16", False, 328), ("f8", True, 144), ("f8", True, 1040), ("f8", True, 2064)])
+def test_workgroups_that_go_on_to_further_tiles(kind, rows_of_k, K):
+    """More tiles of 256 x 256 than compute units, of experts with and without rows."""
+    counts = [(e * 5) % 4 for e in range(800)]
+    counts[400] = 300
+    v = variant(B.grouped_gemm_op(800, sum(counts) + 3, 72, K, rows_of_k, kind, "bf16" if kind == "f8" else kind), 256256)
+    if v is not None:
+        check_grouped(v, counts, 1, 2, 72, K, kind, "bf16" if kind == "f8" else kind, rows_of_k)
+
+
+@pytest.mark.parametrize("kind,rows_of_k,K", [("bf16", True, 40), ("bf16", True, 136), ("f16", False, 200), ("f8", True, 144), ("f8", True, 1168)])
+def test_whole_tiles_in_more_than_one_round(kind, rows_of_k, K):
+    """22 experts of more than half a tile's rows by 18 tiles of columns: 396 whole tiles, a last round too full to be made in quarters; and rests
+    of experts' rows, which are."""
+    counts = [130 + e for e in range(21)] + [256 + 97]
+    v = variant(B.grouped_gemm_op(22, sum(counts) + 3, 4600, K, rows_of_k, kind, "bf16" if kind == "f8" else kind), 256256)
+    if v is not None:
+        check_grouped(v, counts, 1, 2, 4600, K, kind, "bf16" if kind == "f8" else kind, rows_of_k)
+
+
+def test_scaled_whole_tiles_and_quarters():
+    for M, N, K, out in ((2816, 9176, 272, "bf16"), (2900, 6000, 400, "f16")):  # 396 whole tiles; 264 and 24 halves
+        v = variant(B.scaled_gemm_op(M, N, K, out), 256256)
+        if v is None:
+            continue
+        g = rng(M)
+        a, sa, av = f8_and_scales(normal(g, M, K), 1)
+        b, sb, bv = f8_and_scales(normal(g, N, K, scale=0.3), 128)
+        (c,) = launch_twice(v, [dev(x) for x in (a, b, sa, sb)], [((M, N), TYPES[out])])
+        close(c, av @ bv.t(), av.abs() @ bv.abs().t(), K // 64 + 4, out, f8=True)
+
+
+def test_weight_gradients_of_more_tiles_than_compute_units():
+    check_wgrad([(e * 5) % 4 * 17 for e in range(700)], 1, 2, 24, 40, "bf16", "f32", 256256)
+    check_wgrad([(e % 64 == 5) * 100 for e in range(700)], 1, 2, 24, 40, "f16", "f16", 256256)
 
 
 def test_grouped_product_strides():
