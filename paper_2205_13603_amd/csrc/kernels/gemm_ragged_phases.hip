@@ -187,12 +187,12 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         return true;
     };
     // load l of step lk: 0, 1 of A0, 2 to 5 of B, 6, 7 of A1
-    auto load = [&](int l) {
+    auto load = [&](int l, bool inner = false) { // inner: a step that the tile's reduction fills
         const int here = lt.depth - lk * BK;
         const bool of_a = l < 2 || l >= 6;
         const int n = l < 2 ? l : l >= 6 ? l - 4 : l - 2;
         unsigned v = of_a ? va[n] : vb[n];
-        if (here < BK) { // behind the last k
+        if (!inner && here < BK) { // behind the last k
             const int k = of_a ? (A_KC ? chunk * (16 / ES) : a_k + n % 2 * 32) : (B_KC ? chunk * (16 / ES) : b_k + n * 16);
             if (k >= here) v = OUTSIDE;
         }
@@ -288,7 +288,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #endif
     };
     // the products of four row tiles, in M1 with three loads between them
-    auto multiply = [&](int half) {
+    auto multiply = [&](int half, bool inner) {
         __builtin_amdgcn_s_setprio(1);
 #if IN_DT == DT_F8E4M3
                 constexpr int N = TM / 2 * TN, LAG = 3; // results wait for the matrix core while it works on LAG further products
@@ -297,7 +297,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         for (int m = 0; m < N + LAG; ++m) {
             if (m < N) d[m % (LAG + 1)] = mfma(fb[0][m % TN], fa[0][m / TN], f4_t{0, 0, 0, 0});
             __builtin_amdgcn_sched_barrier(0); // the product first
-            if (half == 1 && m % 5 == 3 && m < 15) load(3 + m / 5);
+            if (half == 1 && m % 5 == 3 && m < 15) load(3 + m / 5, inner);
             if (m >= LAG) {
                 const int o = m - LAG;
                 f4_t &sum = acc[half * 4 + o / TN][o % TN];
@@ -314,7 +314,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     acc[half * 4 + i][j] = mfma(fb[q][j], fa[q][i], acc[half * 4 + i][j]);
-                    if (half == 1 && j == 1 && (q * 4 + i) % 3 == 0) load(3 + (q * 4 + i) / 3);
+                    if (half == 1 && j == 1 && (q * 4 + i) % 3 == 0) load(3 + (q * 4 + i) / 3, inner);
                 }
 #endif
         __builtin_amdgcn_s_setprio(0);
@@ -412,36 +412,36 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     for (;;) {
         const int steps = (ct.depth + BK - 1) / BK;
         int k = 0;
-        auto step = [&](auto moves_on) {
+        auto step = [&](auto moves_on, bool inner) {
             if (SCALED && k && k % KB == 0) cchunk ^= 1;
             read_b(rd);
             read_a(rd, 0);
             read_scales(0, k, cchunk);
-            load(6);
-            load(7);
+            load(6, inner);
+            load(7, inner);
             DL_WAIT_VM(KEEP_R0);
             barrier();
-            multiply(0);
+            multiply(0, inner);
             moves_on();
             barrier();
             read_a(rd, 1);
             read_scales(1, k, cchunk);
             load_scales();
-            load(0);
-            load(1);
-            load(2);
+            load(0, inner);
+            load(1, inner);
+            load(2, inner);
             DL_WAIT_VM(KEEP_R1);
             barrier();
-            multiply(1);
+            multiply(1, inner);
             barrier();
             rd ^= 1;
             ++k;
         };
         // the last steps, in which the cursor goes on to the next tile, in a loop of their own: its registers are not the others'
 #pragma unroll 1
-        while (more && lk + 1 < lsteps) step(next_step);
+        while (more && lk + 2 < lsteps) step(next_step, true); // requests of steps lk and lk + 1, neither the tile's last
 #pragma unroll 1
-        while (k < steps) step(advance);
+        while (k < steps) step(advance, false);
         store(ct);
         zero();
         // the next tile of the products: the one that the cursor found
