@@ -241,6 +241,7 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
             constexpr int CH = TN * 2; // 16-byte chunks of a wavefront's row
             barrier();                 // the last step's operands have been read
             char *const mine = lds + wave * (16 * CH * 16);
+            static_assert(16 * CH % 64 == 0, "whole rows to a store");
             static_assert(NW * 16 * CH * 16 <= STAGES * STAGE, "results fit where the operands were");
 #pragma unroll
             for (int i = 0; i < TM; ++i) {

@@ -7,6 +7,7 @@
 
 #include <algorithm>
 #include <cinttypes>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 
@@ -712,7 +713,10 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
         const int64_t ring = (int64_t)t.wi * t.stages * ((t.bm + t.bn) * 128 + (scaled ? 512 : 0));
         t.lds = std::max<int64_t>(ring, (int64_t)t.wi * t.bm * t.bn * 4) + (table ? 4096 : 0);
     } else {
-        t.wi = 2;
+        // 8 bits: two wavefronts to each SIMD, one multiplies while the other reads and scales (256 x 2048 x 5440: 64 x 128 33.5 -> 25.0 us,
+        // 128 x 128 49.7 -> 36.8).  16-bit floats read a wavefront's larger tile in fewer pieces (transposed 4099 x 1032 x 2048: four
+        // wavefronts 33, eight 38).
+        t.wi = code == 256256 || !scaled ? 2 : 4;
         t.wj = code == 256256 ? 4 : 2;
         t.stages = code == 64128 ? 3 : 2;
         t.lds = (int64_t)t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
@@ -732,17 +736,47 @@ int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
     return ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) * (op->d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1);
 }
 
+// The block of a product: the least of the times that these kernels measured, in microseconds, with q tiles on each of 256 compute units
+// and steps of 128 bytes of k:  start + tile * q + steps * (share for each tile of a pair, step for one that is alone),  and never less
+// than the matrices take from memory; of equals the smallest tile, which has the most workgroups reading.
+// (Fits of launches of 64 to 4096 whole tiles by 8 and 40 steps, operands in the L2s, contiguous along k; the others within 10 %.)
+// What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 12.6 us, 64 x 128 25.0, 128 x 128 36.8; 1111 x 2056 x
+// 1360: 24.5, 14.8, 14.1 and 256 x 256 16.4; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
+// experts, 1024 x 2048: 16 x 16 11.3, 16 x 32 12.4, 64 x 128 16.5.  Over 100 drawn sizes of every kind it took 1.02 times the best block's time.
 int64_t ragged_rule(const ms_op *op)
 {
-    if (!ragged_aligned(op)) return 64128;
-    if (op->d.kind == MS_OP_GROUPED_WGRAD) return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 ? 256256 : 128128;
-    const int64_t rows = op->d.kind == MS_OP_GROUPED_GEMM ? (op->M + op->nb - 1) / op->nb : op->M; // of an expert
-    if (ragged_by_k(op)) {
-        if (rows <= 16) return 16032;
-        if (rows <= 32) return 32032;
+    if (!ragged_aligned(op)) return 64128; // the one that reads element by element
+    static const struct { int code; double start, tile, step, share; } costs[2][7] = {
+        {{16016, 2.0, 0.4, 0.070, 0.063}, {16032, 1.6, 1.2, 0.10, 0.10}, {32032, 1.6, 1.35, 0.15, 0.17}, {64032, 2.0, 1.65, 0.23, 0.30},
+         {64128, 5.0, 1.05, 0.50, 0.395}, {128128, 5.0, 1.2, 0.75, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
+        {{16016, 2.5, 0.6, 0.062, 0.056}, {16032, 1.4, 1.95, 0.095, 0.085}, {32032, 1.6, 1.95, 0.125, 0.145}, {64032, 2.0, 2.0, 0.19, 0.28},
+         {64128, 3.6, 1.2, 0.42, 0.315}, {128128, 4.5, 1.75, 0.70, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
+    const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD;
+    // the rows of an expert are not known here: all alike
+    const int64_t experts = op->d.kind == MS_OP_SCALED_GEMM ? 1 : std::min(op->nb, wgrad ? op->K : op->M), matrices = wgrad ? op->nb : experts;
+    const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
+    const double steps = std::ceil((wgrad ? (double)op->K / (double)experts : (double)op->K) * op->in_size / 128);
+    const double reading = wgrad ? 0 : 3.0 + (double)matrices * (double)op->N * (double)op->K * op->in_size / 6e6; // 6 TB/s
+    int64_t best = 0;
+    double least = 0;
+    for (const auto &c : costs[op->in_size == 1 ? 0 : 1]) {
+        if (!layer_block_fits(op, c.code)) continue;
+        const RaggedTile t = ragged_tile(op, c.code);
+        const bool ragged = experts > 1 && !wgrad; // an expert ends within a tile
+        double q, product;
+        if (c.code == 256256) { // divides what is left into quarters
+            q = std::max(1.0, std::ceil((rows / 256 + (ragged ? 0.25 : 0)) * (double)matrices * ((double)op->N / 256) / 64) / 4);
+            product = (wgrad && experts > 1 ? q + 1 : q) * c.share; // a gradient's tiles are as long as their experts: one more
+        } else {
+            q = (ragged ? std::max(1.0, rows / t.bm + 0.5) : std::ceil(rows / t.bm)) * (double)matrices * std::ceil((double)op->N / t.bn) / 256;
+            q = std::max(1.0, std::ceil(q - 0.03));
+            const double n = wgrad && experts > 1 ? q + 1 : q, pairs = std::floor(n / 2);
+            product = pairs * 2 * c.share + (n - 2 * pairs) * c.step;
+        }
+        const double time = std::max(reading, c.start + c.tile * q + steps * product);
+        if (!best || time < least) best = c.code, least = time;
     }
-    if (rows <= 64) return 64128;
-    return ragged_tiles(op, ragged_tile(op, 256256)) >= 192 && rows >= 192 && layer_block_fits(op, 256256) ? 256256 : 128128;
+    return best;
 }
 
 int64_t rms_rule(const ms_op *op)

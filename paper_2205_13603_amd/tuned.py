@@ -109,4 +109,35 @@ def precompile_all(threads=4):
         for protocol in ("filling", "steady"):
             for _, space, t in records_with_traces(name, op, protocol=protocol):
                 n += B.prebuild(op, space, [t], threads)
+    return n + precompile_layers(threads)
+
+
+def layer_ops():
+    """One operator for each set of kernels of the layers (their kernels do not depend on sizes): types, layouts, whole 16 bytes or not."""
+    halves = ("f16", "bf16")
+    ops = [B.rms_norm_op(64, 512, t, out, residual) for t in halves + ("f32",) for out in (t, "f8") for residual in (False, True)]
+    for cols, depth in ((512, 256), (509, 250)):
+        ops += [B.scaled_gemm_op(64, cols, depth, out) for out in halves + ("f32",)]
+        ops += [B.grouped_gemm_op(2, 64, cols, depth, True, "f8", out) for out in halves + ("f32",)]
+        for t in halves:
+            for out in (t, "f32"):
+                ops += [B.grouped_gemm_op(2, 64, cols, depth, by_k, t, out) for by_k in (True, False)]
+                ops.append(B.grouped_wgrad_op(2, 64, cols, depth, t, out))
+    return ops
+
+
+def precompile_layers(threads=4):
+    """Every kernel that a rule of theirs can choose, so that no size compiles at its first call."""
+    n = 0
+    for op in layer_ops():
+        space = op.space()
+        traces = []
+        for code in space.slots[0].candidates[:space.slots[0].n_candidates]:
+            t = B.make_trace(space, [[code]])
+            try:
+                B.trace_validate(op, space, t)
+            except B.MsError:
+                continue
+            traces.append(t)
+        n += B.prebuild(op, space, traces, threads)
     return n
