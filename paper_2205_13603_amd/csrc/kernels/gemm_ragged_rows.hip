@@ -15,7 +15,7 @@ constexpr int LOADS = LA + LB + (SCALED ? 2 : 0), SLOT = (BM + BN) * 128 + (SCAL
 constexpr int RING = NW * STAGES * SLOT, SUMS = NW * BM * BN * 4, TABLE_AT = RING > SUMS ? RING : SUMS;
 constexpr int LDS_BYTES = TABLE_AT + (GROUPED ? 4096 : 0);
 static_assert(LDS_BYTES == LDS_HOST, "the host's count of LDS");
-static_assert(STAGES <= 4 && (STAGES - 1) * LOADS < 64 && BM <= 64 && 128 % BN == 0, "see ragged_tile()");
+static_assert(STAGES <= 2 && (STAGES - 1) * LOADS < 64 && BM <= 64 && 128 % BN == 0, "see ragged_tile()");
 
 extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_args g)
 {
@@ -97,8 +97,6 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     for (int i = 0; i < mine; ++i) {
         const int behind = mine - 1 - i; // blocks whose loads may still be in flight
         if (behind >= STAGES - 1) DL_WAIT_VM((STAGES - 1) * LOADS);
-        else if (STAGES > 3 && behind == 2) DL_WAIT_VM(2 * LOADS);
-        else if (STAGES > 2 && behind == 1) DL_WAIT_VM(LOADS);
         else DL_WAIT_VM(0);
         asm volatile("" ::: "memory");
         const char *p = ring_p + stage * SLOT;

@@ -693,6 +693,13 @@ bool ragged_aligned(const ms_op *op)
     return ragged_by_k(op) ? d.b_strides[2] % n == 0 : op->N % n == 0 && d.b_strides[1] % n == 0;
 }
 
+// row tiles of a launch: of every expert the last may be a part of one
+int64_t ragged_row_tiles(const ms_op *op, int64_t bm)
+{
+    const int64_t experts = op->d.kind == MS_OP_GROUPED_GEMM ? std::min(op->nb, op->M) : 1;
+    return op->d.kind == MS_OP_GROUPED_GEMM ? (op->M - experts) / bm + experts : (op->M + bm - 1) / bm;
+}
+
 struct RaggedTile {
     int bm, bn, wi, wj, stages; // tiles in LDS: wavefronts by rows and columns; few rows: wi = wavefronts that share the reduction
     bool few;
@@ -707,9 +714,13 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
     t.few = t.bn <= 32;
     const bool scaled = op->in_size == 1, table = op->d.kind == MS_OP_GROUPED_GEMM;
     if (t.few) {
-        t.wi = 4;
+        // Where each workgroup has a compute unit to itself, eight wavefronts share its reduction (10 x 256 x 13312 in 8 bits: 9.0 -> 6.6 us,
+        // 256 x 2048 x 5440 by 32 x 32: 16.5 -> 14.5); otherwise four, with rings small enough that several workgroups fit beside each other
+        // (bf16, one row for each of 16 experts, 1024 x 2048: rings of four 11.2, of two 9.75, one 9.8; 64 rows of 8 experts, 2048 x 1024:
+        // 10.8, 9.0, 8.3; 4096 x 14336 of one matrix in 8 bits: 10.8, 11.1, 18.1).
+        t.wi = ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) <= 256 ? 8 : 4;
         t.wj = 1;
-        t.stages = t.bm + t.bn > 64 ? 2 : 4;
+        t.stages = code == 64032 ? 1 : 2;
         const int64_t ring = (int64_t)t.wi * t.stages * ((t.bm + t.bn) * 128 + (scaled ? 512 : 0));
         t.lds = std::max<int64_t>(ring, (int64_t)t.wi * t.bm * t.bn * 4) + (table ? 4096 : 0);
     } else {
@@ -725,12 +736,6 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
     }
     return t;
 }
-// row tiles of a launch: of every expert the last may be a part of one
-int64_t ragged_row_tiles(const ms_op *op, int64_t bm)
-{
-    const int64_t experts = op->d.kind == MS_OP_GROUPED_GEMM ? std::min(op->nb, op->M) : 1;
-    return op->d.kind == MS_OP_GROUPED_GEMM ? (op->M - experts) / bm + experts : (op->M + bm - 1) / bm;
-}
 int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
 {
     return ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) * (op->d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1);
@@ -740,16 +745,16 @@ int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
 // and steps of 128 bytes of k:  start + tile * q + steps * (share for each tile of a pair, step for one that is alone),  and never less
 // than the matrices take from memory; of equals the smallest tile, which has the most workgroups reading.
 // (Fits of launches of 64 to 4096 whole tiles by 8 and 40 steps, operands in the L2s, contiguous along k; the others within 10 %.)
-// What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 12.6 us, 64 x 128 25.0, 128 x 128 36.8; 1111 x 2056 x
-// 1360: 24.5, 14.8, 14.1 and 256 x 256 16.4; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
-// experts, 1024 x 2048: 16 x 16 11.3, 16 x 32 12.4, 64 x 128 16.5.  Over 100 drawn sizes of every kind it took 1.02 times the best block's time.
+// What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 11.9 us, 64 x 128 25.0, 128 x 128 36.8; 1111 x 2056 x
+// 1360: 22.0, 14.8, 14.1 and 256 x 256 16.4; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
+// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 100 drawn sizes of every kind it took 1.02 times the best block's time.
 int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
     static const struct { int code; double start, tile, step, share; } costs[2][7] = {
-        {{16016, 2.0, 0.4, 0.070, 0.063}, {16032, 1.6, 1.2, 0.10, 0.10}, {32032, 1.6, 1.35, 0.15, 0.17}, {64032, 2.0, 1.65, 0.23, 0.30},
+        {{16016, 2.6, 0.0, 0.061, 0.070}, {16032, 2.5, 0.12, 0.089, 0.085}, {32032, 2.5, 0.25, 0.133, 0.148}, {64032, 3.0, 0.0, 0.234, 0.29},
          {64128, 5.0, 1.05, 0.50, 0.395}, {128128, 5.0, 1.2, 0.75, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
-        {{16016, 2.5, 0.6, 0.062, 0.056}, {16032, 1.4, 1.95, 0.095, 0.085}, {32032, 1.6, 1.95, 0.125, 0.145}, {64032, 2.0, 2.0, 0.19, 0.28},
+        {{16016, 3.0, 0.2, 0.051, 0.058}, {16032, 3.0, 0.5, 0.083, 0.069}, {32032, 2.5, 0.75, 0.117, 0.128}, {64032, 3.8, 0.2, 0.196, 0.255},
          {64128, 3.6, 1.2, 0.42, 0.315}, {128128, 4.5, 1.75, 0.70, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
     const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD;
     // the rows of an expert are not known here: all alike
@@ -781,11 +786,15 @@ int64_t ragged_rule(const ms_op *op)
 
 int64_t rms_rule(const ms_op *op)
 {
-    // few rows: a chunk of 8 columns for every lane; many: the four that its registers hold
-    const int64_t chunk = op->M <= 512 ? 512 : 2048;
-    int64_t waves = 1;
-    while (waves < 16 && waves * chunk < op->K) waves *= 2;
-    return waves;
+    // Two chunks of 8 columns for a lane while that leaves ten wavefronts to a compute unit, else the four that its registers hold.
+    // bf16 into 8 bits with a residual, by wavefronts to a row: 128 x 5000 8: 4.8 us, 4: 5.0, 16: 5.3; 613 x 4096 4: 6.2, 2: 7.5;
+    // 613 x 5000 4: 7.3, 8: 8.9; 2048 x 4096 2: 13.0, 4: 13.9; 16384 x 8192 4: 177, 8: 187; 16384 x 16384 8: 351, 16: 411.
+    auto waves = [&](int64_t columns) {
+        int64_t n = 1;
+        while (n < 8 && n * columns < op->K) n *= 2;
+        return n;
+    };
+    return op->M * waves(1024) <= 10 * 256 ? waves(1024) : waves(2048);
 }
 
 // fields of a layer's variant; the limits are checked

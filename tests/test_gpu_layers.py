@@ -195,6 +195,15 @@ def test_grouped_product_of_odd_sizes(kind, rows_of_k, N, K):
         check_grouped(v, counts, 1, 1, N, K, kind, "bf16" if kind == "f8" else kind, rows_of_k)
 
 
+@pytest.mark.parametrize("code", [16016, 16032, 32032, 64032])
+@pytest.mark.parametrize("kind", ["f8", "bf16"])
+def test_few_rows_in_more_workgroups_than_compute_units(kind, code):
+    counts = [70, 0, 1, 33, 3]
+    v = variant(B.grouped_gemm_op(5, sum(counts) + 3, 4200, 656, True, kind, "bf16"), code)
+    if v is not None:
+        check_grouped(v, counts, 1, 2, 4200, 656, kind, "bf16", True)
+
+
 def test_grouped_product_takes_offsets_outside_for_the_nearer_end():
     v = variant(B.grouped_gemm_op(3, 40, 32, 64))
     if v is None:
