@@ -8,11 +8,11 @@
 #include "ragged.h"
 #include "ragged_tile.h"
 
-typedef ragged_tile<TILE_M, TILE_N, TILE_WI, TILE_WJ, TILE_STAGES> tile;
+typedef ragged_tile<TILE_M, TILE_N, TILE_WI, TILE_WJ, TILE_STAGES, TILE_GROUPS> tile;
 constexpr int TABLE_AT = tile::LDS_BYTES, LDS_BYTES = TABLE_AT + (GROUPED && !WGRAD ? 4096 : 0);
 static_assert(LDS_BYTES == LDS_HOST, "the host's count of LDS");
 
-extern "C" __global__ void __launch_bounds__(tile::NW * 64) ms_kernel(const ragged_args g)
+extern "C" __global__ void __launch_bounds__(tile::THREADS) ms_kernel(const ragged_args g)
 {
     __shared__ __attribute__((aligned(1024))) char lds[LDS_BYTES];
     const int lane = threadIdx.x % 64, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), inst = blockIdx.y;

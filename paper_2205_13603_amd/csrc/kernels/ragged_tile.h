@@ -5,22 +5,27 @@
 // lie there as rows of eight 16-byte chunks, swizzled by the row so that a fragment read meets each bank once; the others as rows of
 // k, in 32-byte granules swizzled by k, read with the transposing LDS loads.  What lies behind an expert's rows, the last column or the last
 // k is read as zeros and not stored.
-template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
+//
+// Where a tile has its compute unit to itself GROUPS = 2: two groups of wavefronts take the k steps in turn, each with a ring of its own and
+// half a step behind the other, so that one reads fragments while the other multiplies; in the end each adds up half of the sums.
+template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragged_tile {
     static constexpr int BM = TR, BN = TC, WI = WR, WJ = WC, STAGES = RING, NW = WI * WJ, TM = BM / WI / 16, TN = BN / WJ / 16, BK = 128 / ES;
+    static constexpr int THREADS = NW * GROUPS * 64;
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB; // load instructions of a wavefront and step
     static constexpr bool SCALED = IN_DT == DT_F8E4M3;
     static constexpr int KB = 8;                                              // k blocks whose scales are in LDS at a time, twice
     static constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, SB_BYTES = SCALED ? 256 : 0;
-    static constexpr int SC_AT = STAGES * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LDS_BYTES = SB_AT + 2 * SB_BYTES;
-    static constexpr int LS = SCALED ? KB * BM / 64 / NW : 0;                 // load instructions of a wavefront for the scales of KB blocks
+    static constexpr int SC_AT = GROUPS * STAGES * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LDS_BYTES = SB_AT + 2 * SB_BYTES;
+    static constexpr int LS = SCALED ? KB * BM / 64 / (NW * GROUPS) : 0;                 // load instructions of a wavefront for the scales of KB blocks
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wavefront issues the same loads");
+    static_assert(GROUPS == 1 || (STAGES == 2 && TM % 2 == 0), "two groups: two stages each, half the sums each");
     static_assert(BM >= 64 && 128 % (TN * 16) == 0, "a wavefront's columns share a scale");
 
     // `lds`: LDS_BYTES that no wavefront uses any more
     static __device__ __forceinline__ void make(const ragged_args &g, int inst, const tile_t &t, char *lds)
     {
-        const int tid = threadIdx.x, lane = tid % 64, wave = __builtin_amdgcn_readfirstlane(tid / 64);
+        const int tid = threadIdx.x, lane = tid % 64, every = __builtin_amdgcn_readfirstlane(tid / 64), group = GROUPS > 1 ? every / NW : 0, wave = GROUPS > 1 ? every % NW : every;
         const int wi = wave / WJ, wj = wave % WJ, lrow = lane % 16, lgrp = lane / 16;
         const int cols = g.cols - t.col < BN ? g.cols - t.col : BN;
         const int steps = (t.depth + BK - 1) / BK;
@@ -63,7 +68,7 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
             const bool tail = step * BK + BK > t.depth; // elements of k that there are not
             const int here = t.depth - step * BK;
             const rsrc_t ra = buffer_at(a + (A_KC ? (long)step * 128 : (long)step * BK * g.a_row)), rb = buffer_at(b + (B_KC ? (long)step * 128 : (long)step * BK * g.b_row));
-            const unsigned at = lds0 + stage * STAGE + wave * 1024;
+            const unsigned at = lds0 + (group * STAGES + stage) * STAGE + wave * 1024;
 #pragma unroll
             for (int l = 0; l < LA; ++l) {
                 unsigned v = avoff[l];
@@ -116,10 +121,10 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
             const unsigned at = lds0 + SC_AT + first / KB % 2 * SC_BYTES;
 #pragma unroll
             for (int l = 0; l < LS; ++l) {
-                const int i = wave * LS + l, row = i / KB * 64 + lane, k = i % KB; // the blocks of one line follow each other
+                const int i = every * LS + l, row = i / KB * 64 + lane, k = i % KB; // the blocks of one line follow each other
                 gather_lds4(r, row < t.rows && first + k < blocks ? (unsigned)(row * blocks + k) * 4 : OUTSIDE, at + (k * BM + i / KB * 64) * 4);
             }
-            if (wave == 0) { // columns: lane = 8 * (block of columns) + block of k
+            if (every == 0) { // columns: lane = 8 * (block of columns) + block of k
                 const int n = lane / KB;
                 gather_lds4(buffer_at(sb + first * 4), n < (BN + 127) / 128 && t.col / 128 + n < col_blocks && first + lane % KB < blocks ? (unsigned)(n * blocks + lane % KB) * 4 : OUTSIDE,
                             lds0 + SB_AT + first / KB % 2 * SB_BYTES);
@@ -162,34 +167,18 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
             return f;
         };
         auto frag_a = [&](int stage, int tm, int q) {
-            const char *p = lds + stage * STAGE;
+            const char *p = lds + (group * STAGES + stage) * STAGE;
             return A_KC ? frag_kc(p, (wi * TM + tm) * 16, q) : frag_tr(p, BM, (wi * TM + tm) * 16, q);
         };
         auto frag_b = [&](int stage, int tn, int q) {
-            const char *p = lds + stage * STAGE + A_BYTES;
+            const char *p = lds + (group * STAGES + stage) * STAGE + A_BYTES;
             return B_KC ? frag_kc(p, (wj * TN + tn) * 16, q) : frag_tr(p, BN, (wj * TN + tn) * 16, q);
         };
 
         // ---- the ring
-#if IN_DT == DT_F8E4M3
-        if (steps) load_scales(0);
-#endif
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s)
-            if (s < steps) load(s, s);
-        int stage = 0;
-#pragma unroll 1
-        for (int s = 0; s < steps; ++s) {
-            // this step's loads have landed; those of the steps behind it may be in flight (the few loads of scales among them only
-            // make a wait longer)
-            if (STAGES > 2 && s + STAGES - 2 < steps) DL_WAIT_VM((STAGES - 2) * LOADS);
-            else DL_WAIT_VM(0);
-            barrier();
-#if IN_DT == DT_F8E4M3
-            if (s % KB == 0) load_scales(s + KB); // beyond the last block: zeros
-#endif
-            if (s + STAGES - 1 < steps) load(s + STAGES - 1, stage ? stage - 1 : STAGES - 1);
-            frag_t fa[KQ][TM], fb[KQ][TN];
+        frag_t fa[KQ][TM], fb[KQ][TN];
+        float fs[TM]; // scales of step s
+        auto read = [&](int s, int stage) {
 #pragma unroll
             for (int q = 0; q < KQ; ++q) {
 #pragma unroll
@@ -201,14 +190,26 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
             const float *sc = reinterpret_cast<const float *>(lds + SC_AT + s / KB % 2 * SC_BYTES) + s % KB * BM + wi * TM * 16 + lrow;
             const float sj = reinterpret_cast<const float *>(lds + SB_AT + s / KB % 2 * SB_BYTES)[(t.col % 128 + wj * TN * 16) / 128 * KB + s % KB];
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const float f = sc[i * 16] * sj;
+            for (int i = 0; i < TM; ++i) fs[i] = sc[i * 16] * sj;
+#endif
+        };
+        auto multiply = [&]() {
+#if IN_DT == DT_F8E4M3
+            constexpr int N = TM * TN, LAG = N > 3 ? 3 : N - 1; // results wait for the matrix core while it works on LAG further products
+            f4_t d[LAG + 1];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const f4_t d = mfma(fb[0][j], fa[0][i], f4_t{0, 0, 0, 0});
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) acc[i][j][v] = __builtin_fmaf(d[v], f, acc[i][j][v]);
+            for (int m = 0; m < N + LAG; ++m) {
+                if (m < N) {
+                    d[m % (LAG + 1)] = mfma(fb[0][m % TN], fa[0][m / TN], f4_t{0, 0, 0, 0});
+                    __builtin_amdgcn_sched_barrier(0); // the product first
                 }
+                if (m >= LAG) {
+                    const int o = m - LAG;
+                    f4_t &sum = acc[o / TN][o % TN];
+                    sum = __builtin_elementwise_fma(d[o % (LAG + 1)], f4_t{fs[o / TN], fs[o / TN], fs[o / TN], fs[o / TN]}, sum);
+                    asm volatile("" : "+v"(sum));
+                }
+                __builtin_amdgcn_sched_barrier(0);
             }
 #else
 #pragma unroll
@@ -218,16 +219,94 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fb[q][j], fa[q][i], acc[i][j]);
 #endif
-            stage = stage + 1 == STAGES ? 0 : stage + 1;
+        };
+#if IN_DT == DT_F8E4M3
+        if (steps) load_scales(0);
+#endif
+        if constexpr (GROUPS == 1) {
+#pragma unroll
+            for (int s = 0; s < STAGES - 1; ++s)
+                if (s < steps) load(s, s);
+            int stage = 0;
+#pragma unroll 1
+            for (int s = 0; s < steps; ++s) {
+                // this step's loads have landed; those of the steps behind it may be in flight (the few loads of scales among them only
+                // make a wait longer)
+                if (STAGES > 2 && s + STAGES - 2 < steps) DL_WAIT_VM((STAGES - 2) * LOADS);
+                else DL_WAIT_VM(0);
+                barrier();
+#if IN_DT == DT_F8E4M3
+                if (s % KB == 0) load_scales(s + KB); // beyond the last block: zeros
+#endif
+                if (s + STAGES - 1 < steps) load(s + STAGES - 1, stage ? stage - 1 : STAGES - 1);
+                read(s, stage);
+                multiply();
+                stage = stage + 1 == STAGES ? 0 : stage + 1;
+            }
+        } else {
+            // Group 0 reads step 2 i in phase 2 i and multiplies in the next, group 1 step 2 i + 1 a phase later.  A step's stage is filled again
+            // while its products are made: all wavefronts of the group have read it.
+            const int turns = (steps + 1) / 2, mine = (steps - group + 1) / 2;
+#if ALIGNED
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                if (i < mine) load(group + 2 * i, i);
+            if (mine > 1) DL_WAIT_VM(LOADS);
+            else DL_WAIT_VM(0);
+            barrier();
+            if (group) barrier();
+#pragma unroll 1
+            for (int i = 0; i < turns; ++i) {
+                const int s = group + 2 * i;
+                if (i < mine) read(s, i % 2);
+                barrier();
+                if (i < mine) {
+#if IN_DT == DT_F8E4M3
+                    if (i % (KB / 2) == 0) load_scales(2 * i + KB); // over those of the steps before, which both groups have read
+#endif
+                    const bool further = i + 2 < mine;
+                    if (further) load(s + 4, i % 2);
+                    multiply();
+                    if (further) DL_WAIT_VM(LOADS);
+                    else DL_WAIT_VM(0);
+                }
+                barrier();
+            }
+            if (!group) barrier();
+            // each group's half of the sums: its own and the other's
+            auto of = [&](f4_t one, f4_t zero) { // values, not places: chosen by address the sums would lie in memory
+                f4_t x;
+#pragma unroll
+                for (int v = 0; v < 4; ++v) x[v] = group ? one[v] : zero[v];
+                return x;
+            };
+            char *const other = lds + (1 - group) * (NW * TM / 2 * TN * 1024) + wave * (TM / 2 * TN * 1024) + lane * 16;
+            const char *const here = lds + group * (NW * TM / 2 * TN * 1024) + wave * (TM / 2 * TN * 1024) + lane * 16;
+            static_assert(NW * TM * TN * 1024 + NW * GROUPS * TN * 512 <= GROUPS * STAGES * STAGE, "sums and results fit where the operands were");
+#pragma unroll
+            for (int i = 0; i < TM / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) *reinterpret_cast<f4_t *>(other + (i * TN + j) * 1024) = of(acc[i][j], acc[TM / 2 + i][j]);
+            barrier();
+#pragma unroll
+            for (int i = 0; i < TM / 2; ++i)
+#pragma unroll
+                for (int j = 0; j < TN; ++j) {
+                    const f4_t x = *reinterpret_cast<const f4_t *>(here + (i * TN + j) * 1024), y = of(acc[TM / 2 + i][j], acc[i][j]);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) acc[i][j][v] = y[v] + x[v];
+                }
+#endif
         }
 
         // ---- results
-        constexpr int OS = sizeof(out_t);
+        constexpr int OS = sizeof(out_t), HALF = TM / GROUPS; // row tiles that this wavefront stores
+        const int row0 = (wi * TM + group * HALF) * 16;
         char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
         if constexpr (OS == 4) {
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int r = (wi * TM + i) * 16 + lrow;
+            for (int i = 0; i < HALF; ++i) {
+                const int r = row0 + i * 16 + lrow;
                 if (r < t.rows) {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
@@ -239,12 +318,12 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
         } else {
             // 16 rows at a time by way of LDS, so that a row's columns leave as whole lines
             constexpr int CH = TN * 2; // 16-byte chunks of a wavefront's row
-            barrier();                 // the last step's operands have been read
-            char *const mine = lds + wave * (16 * CH * 16);
+            if (GROUPS == 1) barrier(); // the last step's operands have been read
+            char *const mine = lds + (GROUPS > 1 ? NW * TM * TN * 1024 : 0) + every * (16 * CH * 16); // two groups: behind the sums
             static_assert(16 * CH % 64 == 0, "whole rows to a store");
             static_assert(NW * 16 * CH * 16 <= STAGES * STAGE, "results fit where the operands were");
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
+            for (int i = 0; i < HALF; ++i) {
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     struct { out_t v[4]; } o;
@@ -257,7 +336,7 @@ template <int TR, int TC, int WR, int WC, int RING> struct ragged_tile {
                 for (int l = 0; l < 16 * CH / 64; ++l) {
                     const int r = (l * 64 + lane) / CH, ch = lane % CH;
                     struct __attribute__((aligned(16))) { out_t v[8]; } o = *reinterpret_cast<const decltype(o) *>(mine + (r * CH + (ch ^ r % CH)) * 16);
-                    const int row = (wi * TM + i) * 16 + r, col = wj * TN * 16 + ch * 8;
+                    const int row = row0 + i * 16 + r, col = wj * TN * 16 + ch * 8;
                     if (row < t.rows && col < cols) {
                         char *dst = c + ((long)(t.row + row) * g.cols + t.col + col) * OS;
                         if (col + 8 <= cols) {

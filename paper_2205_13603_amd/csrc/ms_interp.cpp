@@ -702,9 +702,25 @@ int64_t ragged_row_tiles(const ms_op *op, int64_t bm)
 
 struct RaggedTile {
     int bm, bn, wi, wj, stages; // tiles in LDS: wavefronts by rows and columns; few rows: wi = wavefronts that share the reduction
+    int groups;                 // of wi * wj wavefronts, that take the steps in turn
     bool few;
     int64_t lds;
 };
+int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
+{
+    return ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) * (op->d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1);
+}
+
+// Tiles that a launch is expected to make: the rows of an expert are not known here, all alike; one of many ends in half a tile on average.
+double ragged_expected(const ms_op *op, const RaggedTile &t)
+{
+    const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD;
+    const int64_t experts = op->d.kind == MS_OP_GROUPED_GEMM ? std::min(op->nb, op->M) : wgrad ? op->nb : 1;
+    const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
+    const double row_tiles = experts > 1 && !wgrad ? std::max(1.0, rows / t.bm + 0.5) : std::ceil(rows / t.bm);
+    return row_tiles * (double)experts * std::ceil((double)op->N / t.bn);
+}
+
 // The tile that an MS_SLOT_BLOCK code names; its LDS as the kernels lay it out.
 RaggedTile ragged_tile(const ms_op *op, int64_t code)
 {
@@ -712,72 +728,73 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
     t.bm = (int)(code / 1000);
     t.bn = (int)(code % 1000);
     t.few = t.bn <= 32;
+    t.groups = 1;
     const bool scaled = op->in_size == 1, table = op->d.kind == MS_OP_GROUPED_GEMM;
+    const bool alone = ragged_expected(op, t) <= 256; // each workgroup has a compute unit to itself
     if (t.few) {
         // Where each workgroup has a compute unit to itself, eight wavefronts share its reduction (10 x 256 x 13312 in 8 bits: 9.0 -> 6.6 us,
         // 256 x 2048 x 5440 by 32 x 32: 16.5 -> 14.5); otherwise four, with rings small enough that several workgroups fit beside each other
         // (bf16, one row for each of 16 experts, 1024 x 2048: rings of four 11.2, of two 9.75, one 9.8; 64 rows of 8 experts, 2048 x 1024:
         // 10.8, 9.0, 8.3; 4096 x 14336 of one matrix in 8 bits: 10.8, 11.1, 18.1).
-        t.wi = ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) <= 256 ? 8 : 4;
+        t.wi = alone ? 8 : 4;
         t.wj = 1;
         t.stages = code == 64032 ? 1 : 2;
         const int64_t ring = (int64_t)t.wi * t.stages * ((t.bm + t.bn) * 128 + (scaled ? 512 : 0));
         t.lds = std::max<int64_t>(ring, (int64_t)t.wi * t.bm * t.bn * 4) + (table ? 4096 : 0);
     } else {
-        // 8 bits: two wavefronts to each SIMD, one multiplies while the other reads and scales (256 x 2048 x 5440: 64 x 128 33.5 -> 25.0 us,
-        // 128 x 128 49.7 -> 36.8).  16-bit floats read a wavefront's larger tile in fewer pieces (transposed 4099 x 1032 x 2048: four
-        // wavefronts 33, eight 38).
+        // Two workgroups lie on a compute unit.  8 bits: two wavefronts of each to a SIMD, one multiplies while the other reads and scales
+        // (4096 x 4096 x 2048 by 128 x 128: 53.5 -> 47.9 us).  16-bit floats read a wavefront's larger tile in fewer pieces (transposed
+        // 4099 x 1032 x 2048: four wavefronts 33, eight 38).
         t.wi = code == 256256 || !scaled ? 2 : 4;
         t.wj = code == 256256 ? 4 : 2;
         t.stages = code == 64128 ? 3 : 2;
-        t.lds = (int64_t)t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
+        // Workgroups with a compute unit to themselves: two groups, half a step apart (256 x 2048 x 5440, one group and two: 8 bits, 64 x 128
+        // 25.0 and 21.8, 128 x 128 36.8 and 29.4; bf16 37.8 and 31.1, 59.0 and 43.5).
+        if (code != 256256 && alone && ragged_aligned(op)) t.wi = t.wj = t.stages = t.groups = 2;
+        t.lds = (int64_t)t.groups * t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
         if (code == 256256 && op->out_size == 2) t.lds += 8192; // where results are put together as lines
         if (code == 256256 && (table || op->d.kind == MS_OP_GROUPED_WGRAD)) t.lds += 2048; // experts without a whole tile; their order
     }
     return t;
-}
-int64_t ragged_tiles(const ms_op *op, const RaggedTile &t)
-{
-    return ragged_row_tiles(op, t.bm) * ((op->N + t.bn - 1) / t.bn) * (op->d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1);
 }
 
 // The block of a product: the least of the times that these kernels measured, in microseconds, with q tiles on each of 256 compute units
 // and steps of 128 bytes of k:  start + tile * q + steps * (share for each tile of a pair, step for one that is alone),  and never less
 // than the matrices take from memory; of equals the smallest tile, which has the most workgroups reading.
 // (Fits of launches of 64 to 4096 whole tiles by 8 and 40 steps, operands in the L2s, contiguous along k; the others within 10 %.)
-// What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 11.9 us, 64 x 128 25.0, 128 x 128 36.8; 1111 x 2056 x
-// 1360: 22.0, 14.8, 14.1 and 256 x 256 16.4; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
-// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 100 drawn sizes of every kind it took 1.02 times the best block's time.
+// What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 11.9 us, 64 x 128 21.8, 128 x 128 29.4; 1111 x 2056 x
+// 1360: 16.9, 14.5, 13.5 and 256 x 256 15.0; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
+// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 120 drawn sizes of every kind it took 1.01 times the best block's time.
 int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
     static const struct { int code; double start, tile, step, share; } costs[2][7] = {
         {{16016, 2.6, 0.0, 0.061, 0.070}, {16032, 2.5, 0.12, 0.089, 0.085}, {32032, 2.5, 0.25, 0.133, 0.148}, {64032, 3.0, 0.0, 0.234, 0.29},
-         {64128, 5.0, 1.05, 0.50, 0.395}, {128128, 5.0, 1.2, 0.75, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
+         {64128, 4.6, 1.15, 0.46, 0.395}, {128128, 6.0, 1.4, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
         {{16016, 3.0, 0.2, 0.051, 0.058}, {16032, 3.0, 0.5, 0.083, 0.069}, {32032, 2.5, 0.75, 0.117, 0.128}, {64032, 3.8, 0.2, 0.196, 0.255},
-         {64128, 3.6, 1.2, 0.42, 0.315}, {128128, 4.5, 1.75, 0.70, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
-    const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD;
-    // the rows of an expert are not known here: all alike
+         {64128, 3.8, 1.35, 0.375, 0.315}, {128128, 5.2, 1.75, 0.54, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
+    const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD, many = op->d.kind != MS_OP_SCALED_GEMM && op->nb > 1;
     const int64_t experts = op->d.kind == MS_OP_SCALED_GEMM ? 1 : std::min(op->nb, wgrad ? op->K : op->M), matrices = wgrad ? op->nb : experts;
     const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
     const double steps = std::ceil((wgrad ? (double)op->K / (double)experts : (double)op->K) * op->in_size / 128);
-    const double reading = wgrad ? 0 : 3.0 + (double)matrices * (double)op->N * (double)op->K * op->in_size / 6e6; // 6 TB/s
+    const double bytes = wgrad ? 0 : (double)matrices * (double)op->N * (double)op->K * op->in_size;
     int64_t best = 0;
     double least = 0;
     for (const auto &c : costs[op->in_size == 1 ? 0 : 1]) {
         if (!layer_block_fits(op, c.code)) continue;
         const RaggedTile t = ragged_tile(op, c.code);
-        const bool ragged = experts > 1 && !wgrad; // an expert ends within a tile
+        const double more = wgrad && many ? 1 : 0; // a gradient's tiles are as long as their experts: one more
         double q, product;
         if (c.code == 256256) { // divides what is left into quarters
-            q = std::max(1.0, std::ceil((rows / 256 + (ragged ? 0.25 : 0)) * (double)matrices * ((double)op->N / 256) / 64) / 4);
-            product = (wgrad && experts > 1 ? q + 1 : q) * c.share; // a gradient's tiles are as long as their experts: one more
+            q = std::max(1.0, std::ceil((rows / 256 + (many && !wgrad ? 0.25 : 0)) * (double)matrices * ((double)op->N / 256) / 64) / 4);
+            product = (q + more) * c.share;
         } else {
-            q = (ragged ? std::max(1.0, rows / t.bm + 0.5) : std::ceil(rows / t.bm)) * (double)matrices * std::ceil((double)op->N / t.bn) / 256;
-            q = std::max(1.0, std::ceil(q - 0.03));
-            const double n = wgrad && experts > 1 ? q + 1 : q, pairs = std::floor(n / 2);
+            q = std::max(1.0, std::ceil(ragged_expected(op, t) / 256 - 0.03));
+            const double n = q + more, pairs = std::floor(n / 2);
             product = pairs * 2 * c.share + (n - 2 * pairs) * c.step;
         }
+        // 6 TB/s; the row tiles of an expert find most of its matrix in the caches
+        const double reading = 3.0 + bytes / 6e6 * (many ? 0.75 + 0.25 * std::max(1.0, rows / t.bm + 0.5) : 1.0);
         const double time = std::max(reading, c.start + c.tile * q + steps * product);
         if (!best || time < least) best = c.code, least = time;
     }
@@ -827,12 +844,12 @@ int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *tr
         p->block_m = t.bm;
         p->block_n = t.bn;
         p->block_k = 128 / op->in_size;
-        p->waves = t.wi * t.wj;
+        p->waves = t.wi * t.wj * t.groups;
         p->threads = p->waves * 64;
         p->tile_unit[0] = p->tile_unit[1] = 16;
         p->tile_unit[2] = op->in_size == 1 ? 128 : 32;
         p->mfma = MS_MFMA_CODE(16, 16, p->tile_unit[2]);
-        p->acc_per_thread = t.few ? t.bm * t.bn / 64 : t.bm * t.bn / p->threads;
+        p->acc_per_thread = t.few ? t.bm * t.bn / 64 : t.bm * t.bn / (t.wi * t.wj * 64);
         p->vec = p->vec_b = aligned ? 16 / op->in_size : 1;
         p->lds_bytes = (int32_t)t.lds;
         grid = ragged_tiles(op, t);
@@ -859,6 +876,8 @@ uint64_t hash_params(const ms_op *op, const ms_variant_params *p)
         add((uint64_t)ragged_by_k(op));
         add((uint64_t)p->body_tile);
         add((uint64_t)p->vec);
+        add((uint64_t)p->threads);
+        add((uint64_t)p->lds_bytes);
         return h;
     }
     add((uint64_t)d.kind);
@@ -1580,6 +1599,7 @@ int32_t make_kernel_spec(const ms_op *op, const ms_variant_params *p, KernelSpec
             D.push_back(def("TILE_WI", t.wi));
             D.push_back(def("TILE_WJ", t.wj));
             D.push_back(def("TILE_STAGES", t.stages));
+            D.push_back(def("TILE_GROUPS", t.groups));
             D.push_back(def("ALIGNED", p->vec > 1));
         }
         k.template_name = t.few ? "gemm_ragged_rows.hip" : p->body == MS_BODY_RAGGED_PHASES ? "gemm_ragged_phases.hip" : "gemm_ragged.hip";

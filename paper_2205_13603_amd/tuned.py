@@ -116,13 +116,13 @@ def layer_ops():
     """One operator for each set of kernels of the layers (their kernels do not depend on sizes): types, layouts, whole 16 bytes or not."""
     halves = ("f16", "bf16")
     ops = [B.rms_norm_op(64, 512, t, out, residual) for t in halves + ("f32",) for out in (t, "f8") for residual in (False, True)]
-    for cols, depth in ((512, 256), (509, 250), (8448, 256)):  # the last: more workgroups than compute units
-        ops += [B.scaled_gemm_op(64, cols, depth, out) for out in halves + ("f32",)]
-        ops += [B.grouped_gemm_op(2, 64, cols, depth, True, "f8", out) for out in halves + ("f32",)]
+    for rows, cols, depth in ((64, 512, 256), (64, 509, 250), (1024, 8448, 256)):  # the last: more workgroups than compute units
+        ops += [B.scaled_gemm_op(rows, cols, depth, out) for out in halves + ("f32",)]
+        ops += [B.grouped_gemm_op(2, rows, cols, depth, True, "f8", out) for out in halves + ("f32",)]
         for t in halves:
             for out in (t, "f32"):
-                ops += [B.grouped_gemm_op(2, 64, cols, depth, by_k, t, out) for by_k in (True, False)]
-                ops.append(B.grouped_wgrad_op(2, 64, cols, depth, t, out))
+                ops += [B.grouped_gemm_op(2, rows, cols, depth, by_k, t, out) for by_k in (True, False)]
+                ops.append(B.grouped_wgrad_op(2, rows, cols, depth, t, out))
     return ops
 
 

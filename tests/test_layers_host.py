@@ -57,7 +57,10 @@ def test_sizes_do_not_select_code():
         return p.key, B.variant_kernel_text(op, p)
 
     a = key(B.grouped_gemm_op(5, 301, 136, 64))
-    assert a == key(B.grouped_gemm_op(64, 30100, 4096, 1024, a_strides=[0, 2048, 1]))
+    assert a == key(B.grouped_gemm_op(2, 77, 1032, 1024, a_strides=[0, 2048, 1]))
+    # launches of more workgroups than compute units take the kernel of which two fit beside each other
+    b = key(B.grouped_gemm_op(64, 30100, 4096, 1024))
+    assert a[0] != b[0] and b == key(B.grouped_gemm_op(16, 9000, 2048, 512, a_strides=[0, 2048, 1]))
     assert a[0] != key(B.grouped_gemm_op(5, 301, 136, 64, False))[0]
     assert a[0] != key(B.grouped_gemm_op(5, 301, 136, 64, in_dtype="f16"))[0]
     assert a[0] != key(B.grouped_gemm_op(5, 301, 136, 64, out_dtype="f32"))[0]
