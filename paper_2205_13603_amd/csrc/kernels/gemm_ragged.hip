@@ -20,10 +20,16 @@ extern "C" __global__ void __launch_bounds__(tile::THREADS) ms_kernel(const ragg
     int *table = reinterpret_cast<int *>(lds + TABLE_AT);
     tile_t t;
     if (GROUPED && !WGRAD) {
-        if (wave == 0) count_tiles(offsets, g.experts, g.rows, tile::BM, lane, table);
-        barrier();
+        tile_at where;
+        unsigned of;
+        range_t r;
+        const unsigned nt = (unsigned)(g.cols + tile::BN - 1) / tile::BN;
+        if (!find_row_tile(offsets, g.experts, g.rows, tile::BM, nt, blockIdx.x, lane, wave, table, where, of, r)) return;
+        if (!tile_from<tile::BM, tile::BN>(g, where, of, nt, r, t)) return;
+    } else {
+        // products deal runs of tiles to the XCDs, so that the workgroups that run together on one XCD share rows and columns in its L2
+        const unsigned total = tiles_of<tile::BM, tile::BN>(g, table);
+        if (blockIdx.x >= total || !decode<tile::BM, tile::BN>(g, offsets, table, WGRAD ? blockIdx.x : xcd_run<0>(blockIdx.x, total), lane, t)) return;
     }
-    const unsigned total = tiles_of<tile::BM, tile::BN>(g, table);
-    if (blockIdx.x >= total || !find<tile::BM, tile::BN>(g, offsets, table, blockIdx.x, total, lane, t)) return;
     tile::make(g, inst, t, lds);
 }

@@ -27,29 +27,19 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     int expert = 0, row, rows, col;
     {
         tile_at where = {0, 0, (g.rows + BM - 1) / BM};
-        int of, end = g.rows, first = 0;
+        unsigned of;
+        range_t r = {0, g.rows};
         if (GROUPED) {
-            const int *offsets = g.offsets + (long)inst * (g.experts + 1);
             int *table = reinterpret_cast<int *>(lds + TABLE_AT);
-            if (wave == 0) count_tiles(offsets, g.experts, g.rows, BM, lane, table);
-            barrier();
-            const unsigned total = uniform((unsigned)table[g.experts - 1]) * nt;
-            if (blockIdx.x >= total) return;
-            const unsigned f = xcd_run<0>(blockIdx.x, total);
-            where = find_tile(table, g.experts, f / nt, lane);
-            if ((unsigned)where.tile >= (unsigned)where.tiles) return; // offsets that decrease: nothing outside the tensors is touched
-            of = f - (unsigned)(f / nt - where.tile) * nt;
-            const range_t r = rows_of(offsets, where.expert, g.rows);
+            if (!find_row_tile(g.offsets + (long)inst * (g.experts + 1), g.experts, g.rows, BM, nt, blockIdx.x, lane, wave, table, where, of, r)) return;
             expert = where.expert;
-            first = __builtin_amdgcn_readfirstlane(r.first);
-            end = __builtin_amdgcn_readfirstlane(r.last);
         } else {
             of = xcd_run<0>(blockIdx.x, (unsigned)where.tiles * nt);
         }
-        row = first + of % where.tiles * BM;
-        col = of / where.tiles * BN;
-        rows = end - row < BM ? end - row : BM;
-        if (rows <= 0) return; // likewise
+        row = r.first + of % (unsigned)where.tiles * BM;
+        col = of / (unsigned)where.tiles * BN;
+        rows = r.last - row < BM ? r.last - row : BM;
+        if (rows <= 0) return; // offsets that decrease
     }
     const int cols = g.cols - col < BN ? g.cols - col : BN;
     const char *a = g.a + inst * g.a_inst + (long)row * g.a_row, *b = g.b + inst * g.b_inst + expert * g.b_expert + (long)col * g.b_row;

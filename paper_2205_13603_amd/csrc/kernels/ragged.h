@@ -58,6 +58,17 @@ __device__ __forceinline__ range_t rows_of(const int *offsets, int e, int total)
     return {first, last < first ? first : last};
 }
 
+// Sums over the lanes up to and including each: within rows of 16, over the rows of a half, over the halves.
+__device__ __forceinline__ int sums_of_lanes(int n)
+{
+    n += __builtin_amdgcn_update_dpp(0, n, 0x111, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x112, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x114, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x118, 0xf, 0xf, true);
+    n += __builtin_amdgcn_update_dpp(0, n, 0x142, 0xa, 0xf, false);
+    return n + __builtin_amdgcn_update_dpp(0, n, 0x143, 0xc, 0xf, false);
+}
+
 // Tiles of `bm` rows of the experts up to and including e, for all of them, into `table` (LDS): by the first wavefront, before a barrier.
 // Offsets that decrease make ranges overlap: the callers check what they find.
 __device__ __forceinline__ void count_tiles(const int *offsets, int experts, int total, int bm, int lane, int *table)
@@ -70,12 +81,7 @@ __device__ __forceinline__ void count_tiles(const int *offsets, int experts, int
             const range_t r = rows_of(offsets, e, total);
             n = (r.last - r.first + bm - 1) / bm;
         }
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __builtin_amdgcn_ds_bpermute((lane - d) * 4, n);
-            n += lane >= d ? x : 0;
-        }
-        n += before;
+        n = sums_of_lanes(n) + before;
         if (e < experts) table[e] = n;
         before = __builtin_amdgcn_readlane(n, 63);
     }
@@ -96,12 +102,7 @@ __device__ __forceinline__ void count_wide_tiles(const int *offsets, int experts
         }
         const unsigned long m = __ballot(h); // halves of the lanes up to this one
         h = before_h + __builtin_popcountl(m & (~0ul >> (63 - lane)));
-#pragma unroll
-        for (int d = 1; d < 64; d *= 2) {
-            const int x = __builtin_amdgcn_ds_bpermute((lane - d) * 4, n);
-            n += lane >= d ? x : 0;
-        }
-        n += before;
+        n = sums_of_lanes(n) + before;
         if (e < experts) {
             table[e] = n;
             halves[e] = (unsigned short)h;
@@ -129,6 +130,37 @@ template <class T> __device__ __forceinline__ tile_at find_tile(const T *table, 
     }
 }
 
+// For workgroups that make one tile: the expert and row tile of workgroup `block` in launches of `nt` tiles of columns, its place among the
+// expert's tiles (`of`) and the expert's rows; false: past the last tile.  Up to 64 experts fit in the lanes of each wavefront: one load of
+// the offsets and no barrier (8 bits, 43 experts, 647 x 1576 x 768 by 16 x 16: 22.4 us through a table in LDS, 18.1 this way).
+__device__ __forceinline__ bool find_row_tile(const int *offsets, int experts, int total, int bm, unsigned nt, unsigned block, int lane, int wave, int *table, tile_at &where, unsigned &of, range_t &rows)
+{
+    if (experts <= 64) {
+        range_t r = {0, 0};
+        if (lane < experts) r = rows_of(offsets, lane, total);
+        const int n = sums_of_lanes((r.last - r.first + bm - 1) / bm), all = __builtin_amdgcn_readlane(n, 63);
+        if (block >= (unsigned)all * nt) return false;
+        const unsigned f = xcd_run<0>(block, (unsigned)all * nt);
+        const int t = uniform(f / nt), e = __builtin_ctzl(__ballot(n > t));
+        const int from = e ? __builtin_amdgcn_readlane(n, e - 1) : 0, to = __builtin_amdgcn_readlane(n, e);
+        where = {e, t - from, to - from};
+        of = f - (unsigned)from * nt;
+        rows = {__builtin_amdgcn_readlane(r.first, e), __builtin_amdgcn_readlane(r.last, e)};
+        return true;
+    }
+    if (wave == 0) count_tiles(offsets, experts, total, bm, lane, table);
+    barrier();
+    const unsigned all = uniform((unsigned)table[experts - 1]) * nt;
+    if (block >= all) return false;
+    const unsigned f = xcd_run<0>(block, all);
+    where = find_tile(table, experts, (int)(f / nt), lane);
+    if ((unsigned)where.tile >= (unsigned)where.tiles) return false; // offsets that decrease: nothing outside the tensors is touched
+    of = f - (unsigned)(f / nt - where.tile) * nt;
+    rows = rows_of(offsets, where.expert, total);
+    rows = {__builtin_amdgcn_readfirstlane(rows.first), __builtin_amdgcn_readfirstlane(rows.last)};
+    return true;
+}
+
 #ifdef WGRAD // tiles of rows and columns
 struct tile_t {
     int expert, row, rows, col; // first row (of A and C; WGRAD: of D[e]) and how many rows the tile has, first column
@@ -143,8 +175,35 @@ template <int TR, int TC> __device__ __forceinline__ unsigned tiles_of(const rag
     return (unsigned)((g.rows + TR - 1) / TR) * nt * (WGRAD ? (unsigned)g.experts : 1u);
 }
 
-// Tile `f`; false: there is nothing to do (offsets that decrease: nothing outside the tensors is touched).  Of an expert 8 row tiles by all
-// columns at a time, rows first.  WIDE: row tiles as count_wide_tiles counts them.  `order` (WGRAD): the experts in the order in which their
+// The `of`-th tile of an expert (or of the one matrix) with row tiles `where` and rows `r`: 8 row tiles by all columns at a time, rows first.
+// false: it has no rows.
+template <int TR, int TC> __device__ __forceinline__ bool tile_from(const ragged_args &g, const tile_at &where, unsigned of, unsigned nt, const range_t &r, tile_t &t)
+{
+    constexpr unsigned GM = 8;
+    const unsigned band = of / (GM * nt), in = of - band * GM * nt, rest = (unsigned)where.tiles - band * GM, high = rest < GM ? rest : GM;
+    t.expert = where.expert;
+    t.col = (int)(in / high) * TC;
+    t.row = (int)(band * GM + in % high) * TR;
+    t.k0 = 0;
+    t.depth = g.depth;
+    int end = g.rows;
+    if (GROUPED) {
+        const int first = __builtin_amdgcn_readfirstlane(r.first), last = __builtin_amdgcn_readfirstlane(r.last);
+        if (WGRAD) {
+            t.k0 = first;
+            t.depth = last - first;
+        } else {
+            t.row += first;
+            end = last;
+        }
+    }
+    t.rows = end - t.row < TR ? end - t.row : TR;
+    // divisions are made on the vector unit; the tile is the same in all lanes, and its fields belong in scalar registers
+    t = {__builtin_amdgcn_readfirstlane(t.expert), __builtin_amdgcn_readfirstlane(t.row), __builtin_amdgcn_readfirstlane(t.rows), __builtin_amdgcn_readfirstlane(t.col), t.k0, t.depth};
+    return t.rows > 0;
+}
+
+// Tile `f`; false: there is nothing to do (offsets that decrease: nothing outside the tensors is touched).  WIDE: row tiles as count_wide_tiles counts them.  `order` (WGRAD): the experts in the order in which their
 // tiles are made.
 template <int TR, int TC, bool WIDE = false> __device__ __forceinline__ bool decode(const ragged_args &g, const int *offsets, const int *table, unsigned f, int lane, tile_t &t, const unsigned short *order = nullptr)
 {
@@ -163,36 +222,9 @@ template <int TR, int TC, bool WIDE = false> __device__ __forceinline__ bool dec
         if ((unsigned)where.tile >= (unsigned)where.tiles) return false;
         of = f - (f / nt - (unsigned)where.tile) * nt;
     }
-    constexpr unsigned GM = 8;
-    const unsigned band = of / (GM * nt), in = of - band * GM * nt, rest = (unsigned)where.tiles - band * GM, high = rest < GM ? rest : GM;
-    t.expert = where.expert;
-    t.col = (int)(in / high) * TC;
-    t.row = (int)(band * GM + in % high) * TR;
-    t.k0 = 0;
-    t.depth = g.depth;
-    int end = g.rows;
-    if (GROUPED) {
-        const range_t r = rows_of(offsets, t.expert, WGRAD ? g.depth : g.rows);
-        const int first = __builtin_amdgcn_readfirstlane(r.first), last = __builtin_amdgcn_readfirstlane(r.last);
-        if (WGRAD) {
-            t.k0 = first;
-            t.depth = last - first;
-        } else {
-            t.row += first;
-            end = last;
-        }
-    }
-    t.rows = end - t.row < TR ? end - t.row : TR;
-    // divisions are made on the vector unit; the tile is the same in all lanes, and its fields belong in scalar registers
-    t = {__builtin_amdgcn_readfirstlane(t.expert), __builtin_amdgcn_readfirstlane(t.row), __builtin_amdgcn_readfirstlane(t.rows), __builtin_amdgcn_readfirstlane(t.col), t.k0, t.depth};
-    return t.rows > 0;
-}
-
-// Tile `f` of `total` in the order of launch: products deal runs of tiles to the XCDs, so that the workgroups that run together on one XCD
-// share rows and columns in its L2.
-template <int TR, int TC> __device__ __forceinline__ bool find(const ragged_args &g, const int *offsets, const int *table, unsigned f, unsigned total, int lane, tile_t &t)
-{
-    return decode<TR, TC>(g, offsets, table, WGRAD ? f : xcd_run<0>(f, total), lane, t);
+    range_t r = {0, 0};
+    if (GROUPED) r = rows_of(offsets, where.expert, WGRAD ? g.depth : g.rows);
+    return tile_from<TR, TC>(g, where, of, nt, r, t);
 }
 #endif
 

@@ -742,15 +742,16 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
         const int64_t ring = (int64_t)t.wi * t.stages * ((t.bm + t.bn) * 128 + (scaled ? 512 : 0));
         t.lds = std::max<int64_t>(ring, (int64_t)t.wi * t.bm * t.bn * 4) + (table ? 4096 : 0);
     } else {
-        // Two workgroups lie on a compute unit.  8 bits: two wavefronts of each to a SIMD, one multiplies while the other reads and scales
+        // Two workgroups lie on a compute unit, three of 64 x 128 (a third stage would leave two: transposed 4099 x 1032 x 2048 37.1 us, with it
+        // 42.5).  8 bits: two wavefronts of each to a SIMD, one multiplies while the other reads and scales
         // (4096 x 4096 x 2048 by 128 x 128: 53.5 -> 47.9 us).  16-bit floats read a wavefront's larger tile in fewer pieces (transposed
         // 4099 x 1032 x 2048: four wavefronts 33, eight 38).
         t.wi = code == 256256 || !scaled ? 2 : 4;
         t.wj = code == 256256 ? 4 : 2;
-        t.stages = code == 64128 ? 3 : 2;
+        t.stages = 2;
         // Workgroups with a compute unit to themselves: two groups, half a step apart (256 x 2048 x 5440, one group and two: 8 bits, 64 x 128
         // 25.0 and 21.8, 128 x 128 36.8 and 29.4; bf16 37.8 and 31.1, 59.0 and 43.5).
-        if (code != 256256 && alone && ragged_aligned(op)) t.wi = t.wj = t.stages = t.groups = 2;
+        if (code != 256256 && alone && ragged_aligned(op)) t.wi = t.wj = t.groups = 2;
         t.lds = (int64_t)t.groups * t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
         if (code == 256256 && op->out_size == 2) t.lds += 8192; // where results are put together as lines
         if (code == 256256 && (table || op->d.kind == MS_OP_GROUPED_WGRAD)) t.lds += 2048; // experts without a whole tile; their order
@@ -764,15 +765,15 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
 // (Fits of launches of 64 to 4096 whole tiles by 8 and 40 steps, operands in the L2s, contiguous along k; the others within 10 %.)
 // What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 11.9 us, 64 x 128 21.8, 128 x 128 29.4; 1111 x 2056 x
 // 1360: 16.9, 14.5, 13.5 and 256 x 256 15.0; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
-// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 120 drawn sizes of every kind it took 1.01 times the best block's time.
+// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 260 drawn sizes of every kind it took 1.02 times the best block's time.
 int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
     static const struct { int code; double start, tile, step, share; } costs[2][7] = {
-        {{16016, 2.6, 0.0, 0.061, 0.070}, {16032, 2.5, 0.12, 0.089, 0.085}, {32032, 2.5, 0.25, 0.133, 0.148}, {64032, 3.0, 0.0, 0.234, 0.29},
-         {64128, 4.6, 1.15, 0.46, 0.395}, {128128, 6.0, 1.4, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
-        {{16016, 3.0, 0.2, 0.051, 0.058}, {16032, 3.0, 0.5, 0.083, 0.069}, {32032, 2.5, 0.75, 0.117, 0.128}, {64032, 3.8, 0.2, 0.196, 0.255},
-         {64128, 3.8, 1.35, 0.375, 0.315}, {128128, 5.2, 1.75, 0.54, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
+        {{16016, 2.4, 0.3, 0.061, 0.070}, {16032, 2.3, 0.5, 0.089, 0.085}, {32032, 2.4, 0.6, 0.133, 0.148}, {64032, 3.0, 0.6, 0.234, 0.28},
+         {64128, 4.4, 0.85, 0.42, 0.375}, {128128, 6.0, 1.4, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
+        {{16016, 2.5, 0.2, 0.051, 0.060}, {16032, 2.5, 0.4, 0.081, 0.070}, {32032, 2.4, 0.6, 0.116, 0.130}, {64032, 3.2, 0.2, 0.196, 0.25},
+         {64128, 4.2, 0.80, 0.375, 0.31}, {128128, 5.2, 1.75, 0.54, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
     const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD, many = op->d.kind != MS_OP_SCALED_GEMM && op->nb > 1;
     const int64_t experts = op->d.kind == MS_OP_SCALED_GEMM ? 1 : std::min(op->nb, wgrad ? op->K : op->M), matrices = wgrad ? op->nb : experts;
     const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
