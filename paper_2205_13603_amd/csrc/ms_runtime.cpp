@@ -16,6 +16,7 @@
 
 using namespace ms;
 
+struct LoadedKernel;
 struct ms_variant {
     ms_op op;
     ms_variant_params p;
@@ -23,6 +24,7 @@ struct ms_variant {
     std::vector<char> *code; // owned by the cache
     hipModule_t mod;
     hipFunction_t fn;
+    const LoadedKernel *layer; // of a layer: where it was launched last, else null
     hipFunction_t fn_reduce; // second kernel of an rfactor launch, else null
     hipFunction_t fn_many;   // kernel of launches over many instances, else null
     ms_variant *nest;        // MS_BODY_CONV_STEPS: the trace's nest, for operands off 16-byte boundaries (nest_of), else null
@@ -48,6 +50,7 @@ static int32_t build_variant(const ms_op *op, const ms_variant_params &p, ms_var
     v->p = p;
     v->mod = nullptr;
     v->fn = nullptr;
+    v->layer = nullptr;
     v->fn_reduce = nullptr;
     v->fn_many = nullptr;
     v->nest = nullptr;
@@ -238,10 +241,11 @@ extern "C" int32_t ms_prebuild(const ms_op *op, const ms_space *space, const ms_
 
 // Loads the kernels of a variant on device `dev`, the current one: also that of few tiles, whichever a launch takes, so that a
 // variant that has been launched once loads nothing more on that device.
-static int32_t load_layer(ms_variant *v, int dev);
+static int32_t load_layer(ms_variant *v, int dev, const LoadedKernel **loaded);
 static int32_t ensure_loaded(ms_variant *v, int dev)
 {
-    if (is_layer_family(v->p.family)) return load_layer(v, dev);
+    const LoadedKernel *layer;
+    if (is_layer_family(v->p.family)) return load_layer(v, dev, &layer);
     for (ms_variant *second : {v->few, v->fill}) {
         const int32_t rc = second ? ensure_loaded(second, dev) : MS_OK;
         if (rc != MS_OK) return rc;
@@ -273,39 +277,56 @@ static int32_t ensure_loaded(ms_variant *v, int dev)
 }
 
 // Kernels of layers: one code object serves operators of all sizes, so it is loaded once for each device and stays until the process
-// ends; a variant only looks it up.  The variants of a decoding step's many sizes then cost no loading.
+// ends; a variant only looks it up.  The variants of a decoding step's many sizes then cost no loading, and one variant serves several
+// devices and threads at once: what it points to never changes.
 struct LoadedKernel {
     hipModule_t mod;
     hipFunction_t fn;
-    int compute_units;
+    int device, compute_units;
 };
 static std::mutex g_layers_mu;
 static std::map<std::pair<const std::vector<char> *, int>, LoadedKernel> g_layers;
 
-static int32_t load_layer(ms_variant *v, int dev)
+// the kernel on device `dev`, null if it is not loaded there
+static const LoadedKernel *layer_on(ms_variant *v, int dev)
 {
-    if (__atomic_load_n(&v->device, __ATOMIC_ACQUIRE) == dev) return MS_OK;
+    const LoadedKernel *last = __atomic_load_n(&v->layer, __ATOMIC_ACQUIRE);
+    if (last && last->device == dev) return last;
     std::lock_guard<std::mutex> lk(g_layers_mu);
-    auto at = g_layers.find({v->code, dev});
-    if (at == g_layers.end()) {
-        hipDeviceProp_t prop;
-        HIP_TRY(hipGetDeviceProperties(&prop, dev));
-        if (strncmp(prop.gcnArchName, "gfx950", 6) != 0)
-            return fail(MS_ERR_UNSUPPORTED, "device %d is %s; kernels are built for gfx950 only", dev, prop.gcnArchName);
-        if ((size_t)v->p.lds_bytes > prop.sharedMemPerBlock)
-            return fail(MS_ERR_HIP, "variant needs %d bytes of LDS, the device offers %zu per workgroup", v->p.lds_bytes, (size_t)prop.sharedMemPerBlock);
-        LoadedKernel k = {nullptr, nullptr, prop.multiProcessorCount};
-        HIP_TRY(hipModuleLoadData(&k.mod, v->code->data()));
-        const hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
-        if (e != hipSuccess) {
-            (void)hipModuleUnload(k.mod);
-            return fail(MS_ERR_HIP, "hipModuleGetFunction: %s", hipGetErrorString(e));
+    const auto at = g_layers.find({v->code, dev});
+    if (at == g_layers.end()) return nullptr;
+    __atomic_store_n(&v->layer, &at->second, __ATOMIC_RELEASE);
+    return &at->second;
+}
+
+static int32_t load_layer(ms_variant *v, int dev, const LoadedKernel **loaded)
+{
+    if ((*loaded = layer_on(v, dev))) return MS_OK;
+    hipDeviceProp_t prop;
+    HIP_TRY(hipGetDeviceProperties(&prop, dev));
+    if (strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+        return fail(MS_ERR_UNSUPPORTED, "device %d is %s; kernels are built for gfx950 only", dev, prop.gcnArchName);
+    if ((size_t)v->p.lds_bytes > prop.sharedMemPerBlock)
+        return fail(MS_ERR_HIP, "variant needs %d bytes of LDS, the device offers %zu per workgroup", v->p.lds_bytes, (size_t)prop.sharedMemPerBlock);
+    {
+        std::lock_guard<std::mutex> lk(g_layers_mu);
+        if (g_layers.find({v->code, dev}) == g_layers.end()) { // no other thread was quicker
+            LoadedKernel k = {nullptr, nullptr, dev, prop.multiProcessorCount};
+            HIP_TRY(hipModuleLoadData(&k.mod, v->code->data()));
+            const hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
+            bool kept = e == hipSuccess;
+            try {
+                if (kept) g_layers.emplace(std::make_pair(v->code, dev), k);
+            } catch (const std::bad_alloc &) {
+                kept = false;
+            }
+            if (!kept) {
+                (void)hipModuleUnload(k.mod);
+                return e == hipSuccess ? fail(MS_ERR_NOMEM, "ms_variant_launch: out of memory") : fail(MS_ERR_HIP, "hipModuleGetFunction: %s", hipGetErrorString(e));
+            }
         }
-        at = g_layers.emplace(std::make_pair(v->code, dev), k).first;
     }
-    v->fn = at->second.fn;
-    v->compute_units = at->second.compute_units;
-    __atomic_store_n(&v->device, dev, __ATOMIC_RELEASE);
+    *loaded = layer_on(v, dev);
     return MS_OK;
 }
 
@@ -385,10 +406,11 @@ static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *cons
     }
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
-    const int32_t rc = load_layer(v, dev);
+    const LoadedKernel *kernel;
+    const int32_t rc = load_layer(v, dev, &kernel);
     if (rc != MS_OK) return rc;
-    if (v->p.body == MS_BODY_RAGGED_PHASES) gx = (unsigned)std::min<uint64_t>(4ull * gx, (uint64_t)std::max(1, v->compute_units)); // persistent workgroups, of tiles or quarters
-    HIP_TRY(hipModuleLaunchKernel(v->fn, gx, gy, 1, v->spec.block[0], 1, 1, 0, (hipStream_t)stream, args, nullptr));
+    if (v->p.body == MS_BODY_RAGGED_PHASES) gx = (unsigned)std::min<uint64_t>(4ull * gx, (uint64_t)std::max(1, kernel->compute_units)); // persistent workgroups, of tiles or quarters
+    HIP_TRY(hipModuleLaunchKernel(kernel->fn, gx, gy, 1, v->spec.block[0], 1, 1, 0, (hipStream_t)stream, args, nullptr));
     return MS_OK;
 }
 
@@ -479,8 +501,9 @@ extern "C" int32_t ms_variant_launch_static(ms_variant *v, const void *const *in
     int dev = 0;
     HIP_TRY(hipGetDevice(&dev));
     ms_variant *run = v;
-    if (!is_layer_family(v->p.family) && inputs[0] && (v->p.family == MS_FAM_REDUCE || inputs[1])) (void)runs(v, inputs, instances, false, &run);
-    if (v->device != dev || !v->fn || !run || run->device != dev || !run->fn)
+    const bool layer = is_layer_family(v->p.family);
+    if (!layer && inputs[0] && (v->p.family == MS_FAM_REDUCE || inputs[1])) (void)runs(v, inputs, instances, false, &run);
+    if (layer ? !layer_on(v, dev) : v->device != dev || !v->fn || !run || run->device != dev || !run->fn)
         return fail(MS_ERR_BAD_ARG, "ms_variant_launch_static: call ms_variant_prepare on device %d first (loading a kernel allocates)", dev);
     const size_t need = workspace_per_instance(v) * (size_t)instances;
     if (need > (size_t)MS_STATIC_WORKSPACE_BYTES)

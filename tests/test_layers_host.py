@@ -1,5 +1,8 @@
 """Layers of language models on the host: what is accepted and refused, the tiles that the rules choose, coverage, the trace that leaves
 all decisions to them.  No GPU."""
+import os
+import subprocess
+
 import numpy as np
 import pytest
 
@@ -184,3 +187,19 @@ def test_search_on_a_synthetic_latency_finds_the_block():
     res = B.search(op, op.space(), cfg, fake_latency=lambda p: 1.0 + abs(p.body_tile - 128128) / 1e5)
     p = B.trace_validate(op, op.space(), res.best_trace)
     assert p.body_tile == 128128
+
+
+def test_launches_on_several_threads_and_devices(tmp_path):
+    """Launches on a stand-in for HIP that keeps book of modules and devices, under the thread sanitizer: each call runs the kernel of its own
+    device, loaded once, and what is not there or not aligned is refused before anything is launched."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "ms_layers")
+    srcs = [os.path.join(root, "paper_2205_13603_amd", "csrc", f) for f in ("ms_core.cpp", "ms_interp.cpp", "ms_model.cpp", "ms_search.cpp", "ms_runtime.cpp")]
+    r = subprocess.run(["g++", "-std=c++17", "-g", "-O1", "-fsanitize=thread", "-D__HIP_PLATFORM_AMD__", "-D__align__(n)=", "-DHIP_SYMBOL(x)=(&x)", "-I", "/opt/rocm/include",
+                        "-o", exe] + srcs + [os.path.join(root, "tests", "sanitize", "layer_driver.cpp"), "-lm", "-lpthread"],
+                       stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
+    assert r.returncode == 0, r.stdout[-4000:]
+    env = dict(os.environ)
+    env.pop("LD_PRELOAD", None)
+    r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env, timeout=600)
+    assert r.returncode == 0 and "layer checks ok" in r.stdout, r.stdout[-6000:]
