@@ -153,6 +153,6 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             for (int v = 0; v < 4; ++v) sum[v] += x[v];
         }
         const int r = tile / NC * 16 + lrow, j = tile % NC * 16 + lgrp * 4;
-        if (r < rows && j < cols) store4(c + ((long)(row + r) * g.cols + col + j) * (long)sizeof(out_t), sum, cols - j);
+        if (r < rows && j < cols) store4<false>(c + ((long)(row + r) * g.cols + col + j) * (long)sizeof(out_t), sum, cols - j);
     }
 }

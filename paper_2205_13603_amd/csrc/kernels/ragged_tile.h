@@ -311,7 +311,7 @@ template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragge
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const int col = (wj * TN + j) * 16 + lgrp * 4;
-                        if (col < cols) store4(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, acc[i][j], cols - col);
+                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, acc[i][j], cols - col);
                     }
                 }
             }
@@ -340,8 +340,7 @@ template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragge
                     if (row < t.rows && col < cols) {
                         char *dst = c + ((long)(t.row + row) * g.cols + t.col + col) * OS;
                         if (col + 8 <= cols) {
-                            struct __attribute__((packed, aligned(2))) any_t { out_t v[8]; };
-                            *reinterpret_cast<any_t *>(dst) = __builtin_bit_cast(any_t, o);
+                            stream_out(dst, o);
                         } else {
 #pragma unroll
                             for (int v = 0; v < 8; ++v)

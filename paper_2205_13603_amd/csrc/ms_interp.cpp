@@ -804,15 +804,16 @@ int64_t ragged_rule(const ms_op *op)
 
 int64_t rms_rule(const ms_op *op)
 {
-    // Two chunks of 8 columns for a lane while that leaves ten wavefronts to a compute unit, else the four that its registers hold.
-    // bf16 into 8 bits with a residual, by wavefronts to a row: 128 x 5000 8: 4.8 us, 4: 5.0, 16: 5.3; 613 x 4096 4: 6.2, 2: 7.5;
-    // 613 x 5000 4: 7.3, 8: 8.9; 2048 x 4096 2: 13.0, 4: 13.9; 16384 x 8192 4: 177, 8: 187; 16384 x 16384 8: 351, 16: 411.
+    // Two chunks of 8 columns for a lane while that leaves ten wavefronts to a compute unit, else the four that its registers hold (fp32:
+    // between two and three).  bf16 into 8 bits with a residual, by wavefronts to a row: 128 x 5000 8: 4.8 us, 4: 5.2, 16: 5.3; 613 x 4096
+    // 4: 5.4, 2: 6.8; 613 x 5000 4: 7.1, 8: 8.4; 2048 x 4096 2: 12.5, 4: 12.8; 16384 x 8192 4: 171, 8: 176; 16384 x 16384 8: 333, 4: 372.
+    // fp32: 2048 x 4096 4: 23.9, 2: 25.9; 16384 x 8192 8: 385, 4: 413; 613 x 5000 4: 9.7, 8: 10.9.
     auto waves = [&](int64_t columns) {
         int64_t n = 1;
         while (n < 8 && n * columns < op->K) n *= 2;
         return n;
     };
-    return op->M * waves(1024) <= 10 * 256 ? waves(1024) : waves(2048);
+    return op->M * waves(1024) <= 10 * 256 ? waves(1024) : waves(op->in_size == 4 ? 1280 : 2048);
 }
 
 // fields of a layer's variant; the limits are checked
