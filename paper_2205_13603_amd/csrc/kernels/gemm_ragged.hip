@@ -3,7 +3,11 @@
 //   C[t][j]    = sum_k A[t][k] B[e(t)][k][j]        8-bit floats: sum over blocks of 128 k of SA[t][b] SB[e][j/128][b] (block's sum)
 //   D[e][i][j] = sum over the rows t of e of P[t][i] Q[t][j]                                                     (WGRAD)
 //
-// A workgroup makes one tile of rows of one expert (ragged_tile.h).
+// A workgroup makes one tile of rows of one expert (ragged_tile.h).  Two or three lie on a compute unit and overlap each other's loads, products
+// and stores; launches that leave each one alone take the steps in two groups instead.  What bounds it is the way from the L2 into LDS,
+// 31 to 46 bytes a clock and compute unit, on top of which come the reads of fragments that no products cover.  Measured: 1111 x 2056 x 1360
+// in 8 bits by 128 x 128 12.5 us (153 workgroups, 0.50 PFLOP/s); f16, 4062 rows of 13 experts, 1032 x 2048, transposed 32.6 (0.53); gradient
+// of 19 experts, 1489 rows, 1032 x 520 by 64 x 128 12.9, of which it writes 26 MB.
 #include "common.h"
 #include "ragged.h"
 #include "ragged_tile.h"

@@ -6,6 +6,8 @@
 // turn, and add their sums up in LDS at the end, in the order of their numbers.  Each has a ring of LDS stages of its own, which
 // loads fill directly and only it reads: no barrier ahead of the end, no registers for data in flight, and eight lanes of a load take a
 // whole line (fragments loaded as the matrix cores take them touch 16 rows with 64 lanes and cost four times the address lookups).
+// Measured: bf16, 16 rows of 12 experts, 1024 x 2048 by 16 x 16 9.4 us, 5.4 TB/s; 8 bits, 4 x 4096 x 4096 5.0, of which the launch is 4;
+// 16 x 8192 x 8192 11.9, 5.6 TB/s.
 #include "common.h"
 #include "ragged.h"
 

@@ -8,6 +8,8 @@
 //
 // Where a tile has its compute unit to itself GROUPS = 2: two groups of wavefronts take the k steps in turn, each with a ring of its own and
 // half a step behind the other, so that one reads fragments while the other multiplies; in the end each adds up half of the sums.
+// (128 x 128 alone on its compute unit, a step: 8 bits 0.75 us with one group, 0.60 with two, 0.40 without products or without loads; 16 bits
+// 0.70, 0.54, 0.40 and 0.35.)
 template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragged_tile {
     static constexpr int BM = TR, BN = TC, WI = WR, WJ = WC, STAGES = RING, NW = WI * WJ, TM = BM / WI / 16, TN = BN / WJ / 16, BK = 128 / ES;
     static constexpr int THREADS = NW * GROUPS * 64;

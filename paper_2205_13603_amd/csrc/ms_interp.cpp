@@ -770,10 +770,10 @@ int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
     static const struct { int code; double start, tile, step, share; } costs[2][7] = {
-        {{16016, 2.4, 0.3, 0.061, 0.070}, {16032, 2.3, 0.5, 0.089, 0.085}, {32032, 2.4, 0.6, 0.133, 0.148}, {64032, 3.0, 0.6, 0.234, 0.28},
-         {64128, 4.4, 0.85, 0.42, 0.375}, {128128, 6.0, 1.4, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
+        {{16016, 2.4, 0.3, 0.061, 0.070}, {16032, 2.3, 0.5, 0.089, 0.085}, {32032, 2.4, 0.6, 0.133, 0.155}, {64032, 2.9, 0.6, 0.234, 0.235},
+         {64128, 4.4, 0.85, 0.42, 0.375}, {128128, 5.7, 1.0, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
         {{16016, 2.5, 0.2, 0.051, 0.060}, {16032, 2.5, 0.4, 0.081, 0.070}, {32032, 2.4, 0.6, 0.116, 0.130}, {64032, 3.2, 0.2, 0.196, 0.25},
-         {64128, 4.2, 0.80, 0.375, 0.31}, {128128, 5.2, 1.75, 0.54, 0.48}, {256256, 4.0, 10.5, 1.40, 1.45}}};
+         {64128, 4.2, 0.80, 0.375, 0.31}, {128128, 4.9, 1.6, 0.54, 0.48}, {256256, 4.0, 9.8, 1.40, 1.45}}};
     const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD, many = op->d.kind != MS_OP_SCALED_GEMM && op->nb > 1;
     const int64_t experts = op->d.kind == MS_OP_SCALED_GEMM ? 1 : std::min(op->nb, wgrad ? op->K : op->M), matrices = wgrad ? op->nb : experts;
     const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
@@ -786,8 +786,9 @@ int64_t ragged_rule(const ms_op *op)
         const RaggedTile t = ragged_tile(op, c.code);
         const double more = wgrad && many ? 1 : 0; // a gradient's tiles are as long as their experts: one more
         double q, product;
-        if (c.code == 256256) { // divides what is left into quarters
-            q = std::max(1.0, std::ceil((rows / 256 + (many && !wgrad ? 0.25 : 0)) * (double)matrices * ((double)op->N / 256) / 64) / 4);
+        if (c.code == 256256) { // divides what is left into quarters, which take 0.4 of a tile's time: all of an expert of few rows
+            const double quarters = many && !wgrad && rows < 256 ? 1.6 : 1;
+            q = std::max(1.0, std::ceil((rows / 256 + (many && !wgrad ? 0.25 : 0)) * quarters * (double)matrices * ((double)op->N / 256) / 64) / 4);
             product = (q + more) * c.share;
         } else {
             q = std::max(1.0, std::ceil(ragged_expected(op, t) / 256 - 0.03));
