@@ -262,6 +262,20 @@ def test_weight_gradients_of_more_tiles_than_compute_units():
     check_wgrad([(e % 64 == 5) * 100 for e in range(700)], 1, 2, 24, 40, "f16", "f16", 256256)
 
 
+@pytest.mark.parametrize("code", [64128, 128128])
+def test_tiles_of_which_several_lie_on_a_compute_unit(code):
+    """More tiles than compute units: the kernels of one group of wavefronts; and at most as many, of two groups, at depths of one step and of an odd and an
+    even number of steps."""
+    counts = [130 + e for e in range(10)] + [0, 97]
+    for kind, rows_of_k, K, N in (("bf16", True, 136, 4600), ("f16", False, 200, 4600), ("f8", True, 1168, 4600), ("bf16", True, 64, 264), ("bf16", True, 192, 264), ("f16", False, 256, 264),
+                                  ("f8", True, 128, 264), ("f8", True, 1168, 264), ("f8", True, 2192, 264)):
+        v = variant(B.grouped_gemm_op(len(counts), sum(counts) + 3, N, K, rows_of_k, kind, "bf16" if kind == "f8" else kind), code)
+        if v is not None:
+            check_grouped(v, counts, 1, 2, N, K, kind, "bf16" if kind == "f8" else kind, rows_of_k)
+    check_wgrad([65, 0, 130, 1] * 6, 1, 2, 264, 520, "bf16", "f32", code)
+    check_wgrad([65, 0, 130, 1] * 6, 1, 2, 264, 520, "f16", "f16", code)
+
+
 def test_grouped_product_strides():
     E, T, N, K = 3, 50, 40, 64
     v = variant(B.grouped_gemm_op(E, T, N, K, True, "bf16", a_strides=[0, 72, 1], b_strides=[44 * 80, 1, 80]))
