@@ -294,6 +294,65 @@ def test_grouped_product_strides():
     close(c, torch.cat([av[:20] @ bv[0], av[20:] @ bv[2]]), torch.cat([av[:20].abs() @ bv[0].abs(), av[20:].abs() @ bv[2].abs()]), K, "bf16")
 
 
+@pytest.mark.parametrize("code", [16016, 64128, 128128, 256256])
+def test_products_beyond_4_gib(code):
+    """The last experts of matrices of 5 GiB, and the last rows of inputs of 5 GiB."""
+    E, N, K = 80, 4096, 8192
+    many, long = variant(B.grouped_gemm_op(E, 40, N, K, True, "bf16", "f32"), code), variant(B.grouped_gemm_op(2, 330000, 128, K, True, "bf16", "f32"), code)
+    if many is None:
+        return
+    g = rng(61)
+    a, last = normal(g, 40, K).bfloat16(), normal(g, N, K).bfloat16()
+    b = torch.zeros(E, N, K, dtype=torch.bfloat16, device="cuda")
+    b[-1] = dev(last)
+    c = torch.full((40, N), 7.0, device="cuda")
+    da, off = dev(a), dev(offsets_of([0] * 30 + [3] + [0] * (E - 33) + [7, 30]))
+    many.launch([da.data_ptr(), b.data_ptr(), off.data_ptr()], c.data_ptr(), stream=devmem.current_stream())
+    torch.cuda.synchronize()
+    assert bool((c[:10] == 0).all())
+    some = slice(0, N, 97)
+    close(c[10:].cpu()[:, some], a[10:].double() @ last[some].double().t(), a[10:].double().abs() @ last[some].double().abs().t(), K, "f32")
+    del b
+    x = torch.zeros(330000, K, dtype=torch.bfloat16, device="cuda")
+    x[-40:] = da
+    w = normal(g, 2, 128, K).bfloat16()
+    c, dw, off = torch.full((330000, 128), 7.0, device="cuda"), dev(w), dev(torch.tensor([330000 - 40, 330000 - 25, 330000], dtype=torch.int32))
+    long.launch([x.data_ptr(), dw.data_ptr(), off.data_ptr()], c.data_ptr(), stream=devmem.current_stream())
+    torch.cuda.synchronize()
+    assert bool((c[:-40] == 7).all())
+    av, wv = a.double(), w.double()
+    close(c[-40:].cpu(), torch.cat([av[:15] @ wv[0].t(), av[15:] @ wv[1].t()]), torch.cat([av[:15].abs() @ wv[0].abs().t(), av[15:].abs() @ wv[1].abs().t()]), K, "f32")
+
+
+@pytest.mark.parametrize("code", [64128, 128128, 256256])
+def test_weight_gradients_and_norms_beyond_4_gib(code):
+    E, I, J = 20, 8192, 8192
+    v, n = variant(B.grouped_wgrad_op(E, 70, I, J, "bf16", "f32"), code), variant(B.rms_norm_op(330000, 8192, "bf16", "f8", residual=False))
+    if v is None:
+        return
+    g = rng(62)
+    p, q = normal(g, 70, I).bfloat16(), normal(g, 70, J).bfloat16()
+    d, dp, dq = torch.full((E, I, J), 7.0, device="cuda"), dev(p), dev(q)
+    off = dev(offsets_of([0] * (E - 2) + [5, 65]))
+    v.launch([dp.data_ptr(), dq.data_ptr(), off.data_ptr()], d.data_ptr(), stream=devmem.current_stream())
+    torch.cuda.synchronize()
+    assert bool((d[:-2] == 0).all())
+    some = slice(0, J, 101)
+    close(d[-1, :, some].cpu(), p[5:].double().t() @ q[5:, some].double(), p[5:].double().abs().t() @ q[5:, some].double().abs(), 65, "f32")
+    del d
+    if code == 64128:
+        x = torch.zeros(330000, 8192, dtype=torch.bfloat16, device="cuda")
+        x[-1] = dp[0]
+        w, y, s = torch.ones(8192, dtype=torch.bfloat16, device="cuda"), torch.full((330000, 8192), 0x55, dtype=torch.uint8, device="cuda"), torch.empty(330000, 64, device="cuda")
+        n.launch([x.data_ptr(), w.data_ptr()], [y.data_ptr(), s.data_ptr(), None], stream=devmem.current_stream())
+        torch.cuda.synchronize()
+        assert bool((y[:-1] == 0).all())
+        yv = p[0].double() / (p[0].double().square().mean() + 1e-6).sqrt()
+        wide = s[-1].cpu().double().repeat_interleave(128)
+        got = y[-1].cpu().view(TYPES["f8"]).double() * wide
+        assert bool(((got - yv).abs() <= yv.abs() * (HALF_STEP["f8"] + 1e-5) * 1.01 + wide * 2.0 ** -10 * 1.01).all())
+
+
 def test_infinities_and_nan_stay_in_their_rows():
     v = variant(B.grouped_gemm_op(2, 40, 64, 128, True, "bf16"))
     if v is None:
@@ -438,6 +497,21 @@ def test_rms_norm_in_place_strided_and_several_instances():
     torch.cuda.synchronize()
     _, yv = rms_definition(x, w[:, None], None, 1e-6, "f16")
     assert bool(((o.cpu().double() - yv).abs() <= yv.abs() * 2.0 ** -11 * 1.02 + 2.0 ** -25).all())
+
+
+@pytest.mark.parametrize("M,N,code", [((4 << 20) + 9, 16, 1), ((1 << 20) + 300, 72, 4)])
+def test_rms_norm_of_more_rows_than_workgroups(M, N, code):
+    v = variant(B.rms_norm_op(M, N, "bf16"), code)
+    if v is None:
+        return
+    g = torch.Generator(device="cuda").manual_seed(71)
+    x, r, w = (torch.randn(*s, generator=g, device="cuda").bfloat16() for s in ((M, N), (M, N), (N,)))
+    y, h = torch.empty_like(x), torch.empty_like(x)
+    v.launch([x.data_ptr(), w.data_ptr(), r.data_ptr()], [y.data_ptr(), None, h.data_ptr()], stream=devmem.current_stream())
+    hv = (x.float() + r.float()).bfloat16()
+    assert torch.equal(h, hv)
+    yv = hv.double() * (hv.double().square().mean(1, keepdim=True) + 1e-6).rsqrt() * w.double()
+    assert bool(((y.double() - yv).abs() <= yv.abs() * 2.0 ** -8 * 1.01 + 1e-37).all())
 
 
 def test_rms_norm_of_zeros_nan_and_large_values():
