@@ -12,7 +12,7 @@
 #include "ragged.h"
 #include "ragged_tile.h"
 
-typedef ragged_tile<TILE_M, TILE_N, TILE_WI, TILE_WJ, TILE_STAGES, TILE_GROUPS> tile;
+typedef ragged_tile<TILE_M, TILE_N, TILE_WI, TILE_WJ, TILE_GROUPS> tile;
 constexpr int TABLE_AT = tile::LDS_BYTES, LDS_BYTES = TABLE_AT + (GROUPED && !WGRAD ? 4096 : 0);
 static_assert(LDS_BYTES == LDS_HOST, "the host's count of LDS");
 

@@ -31,7 +31,7 @@ constexpr int KB = 8, LS = KB * BM / 64 / NW; // k blocks whose scales are in LD
 constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, SB_BYTES = SCALED ? 256 : 0, OS = sizeof(out_t);
 constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, OUT_AT = SB_AT + 2 * SB_BYTES, TABLE_AT = OUT_AT + (OS == 2 ? NW * 1024 : 0);
 constexpr int LDS_BYTES = TABLE_AT + (WGRAD ? 2048 : GROUPED ? 4096 + 2048 : 0);
-typedef ragged_tile<128, 128, 2, 2, 2, 2> quarter;
+typedef ragged_tile<128, 128, 2, 2, 2> quarter;
 static_assert(quarter::LDS_BYTES <= TABLE_AT, "quarters lie where whole tiles did");
 constexpr unsigned QUARTER = 40; // time of a quarter in hundredths of a whole tile's (8 bits, 4096 deep: 26.6 us of 68; bf16: 42 of 105)
 static_assert(LDS_BYTES == LDS_HOST, "the host's count of LDS");

@@ -1,5 +1,5 @@
 // One tile of a product over rows by expert, or of the gradient of the experts' matrices, by all wavefronts of a workgroup: TR rows by TC columns,
-// WR by WC wavefronts, ring of STAGES.
+// WR by WC wavefronts of a group, two stages of LDS.
 //
 // k steps of 128 bytes of each row of the operands go straight into a ring of LDS stages; operands contiguous along k (A_KC, B_KC)
 // lie there as rows of eight 16-byte chunks, swizzled by the row so that a fragment read meets each bank once; the others as rows of
@@ -10,8 +10,8 @@
 // half a step behind the other, so that one reads fragments while the other multiplies; in the end each adds up half of the sums.
 // (128 x 128 alone on its compute unit, a step: 8 bits 0.75 us with one group, 0.60 with two, 0.40 without products or without loads; 16 bits
 // 0.70, 0.54, 0.40 and 0.35.)
-template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragged_tile {
-    static constexpr int BM = TR, BN = TC, WI = WR, WJ = WC, STAGES = RING, NW = WI * WJ, TM = BM / WI / 16, TN = BN / WJ / 16, BK = 128 / ES;
+template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
+    static constexpr int BM = TR, BN = TC, WI = WR, WJ = WC, STAGES = 2, NW = WI * WJ, TM = BM / WI / 16, TN = BN / WJ / 16, BK = 128 / ES;
     static constexpr int THREADS = NW * GROUPS * 64;
     static constexpr int A_BYTES = BM * 128, B_BYTES = BN * 128, STAGE = A_BYTES + B_BYTES;
     static constexpr int LA = BM / 8 / NW, LB = BN / 8 / NW, LOADS = LA + LB; // load instructions of a wavefront and step
@@ -21,7 +21,7 @@ template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragge
     static constexpr int SC_AT = GROUPS * STAGES * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LDS_BYTES = SB_AT + 2 * SB_BYTES;
     static constexpr int LS = SCALED ? KB * BM / 64 / (NW * GROUPS) : 0;                 // load instructions of a wavefront for the scales of KB blocks
     static_assert(BM % (8 * NW) == 0 && BN % (8 * NW) == 0, "every wavefront issues the same loads");
-    static_assert(GROUPS == 1 || (STAGES == 2 && TM % 2 == 0), "two groups: two stages each, half the sums each");
+    static_assert(GROUPS == 1 || TM % 2 == 0, "two groups: half the sums each");
     static_assert(BM >= 64 && 128 % (TN * 16) == 0, "a wavefront's columns share a scale");
 
     // `lds`: LDS_BYTES that no wavefront uses any more
@@ -226,24 +226,17 @@ template <int TR, int TC, int WR, int WC, int RING, int GROUPS = 1> struct ragge
         if (steps) load_scales(0);
 #endif
         if constexpr (GROUPS == 1) {
-#pragma unroll
-            for (int s = 0; s < STAGES - 1; ++s)
-                if (s < steps) load(s, s);
-            int stage = 0;
+            if (steps) load(0, 0);
 #pragma unroll 1
             for (int s = 0; s < steps; ++s) {
-                // this step's loads have landed; those of the steps behind it may be in flight (the few loads of scales among them only
-                // make a wait longer)
-                if (STAGES > 2 && s + STAGES - 2 < steps) DL_WAIT_VM((STAGES - 2) * LOADS);
-                else DL_WAIT_VM(0);
+                DL_WAIT_VM(0); // this step's loads have landed; the barrier: everyone's, and the other stage has been read
                 barrier();
 #if IN_DT == DT_F8E4M3
                 if (s % KB == 0) load_scales(s + KB); // beyond the last block: zeros
 #endif
-                if (s + STAGES - 1 < steps) load(s + STAGES - 1, stage ? stage - 1 : STAGES - 1);
-                read(s, stage);
+                if (s + 1 < steps) load(s + 1, (s + 1) % 2);
+                read(s, s % 2);
                 multiply();
-                stage = stage + 1 == STAGES ? 0 : stage + 1;
             }
         } else {
             // Group 0 reads step 2 i in phase 2 i and multiplies in the next, group 1 step 2 i + 1 a phase later.  A step's stage is filled again

@@ -1601,7 +1601,6 @@ int32_t make_kernel_spec(const ms_op *op, const ms_variant_params *p, KernelSpec
             D.push_back(def("TILE_N", t.bn));
             D.push_back(def("TILE_WI", t.wi));
             D.push_back(def("TILE_WJ", t.wj));
-            D.push_back(def("TILE_STAGES", t.stages));
             D.push_back(def("TILE_GROUPS", t.groups));
             D.push_back(def("ALIGNED", p->vec > 1));
         }
