@@ -18,16 +18,18 @@
 // gradient of 8 experts, 4096 x 2048 into fp32 177 to 181 (0.77 and 2.0 TB/s).
 //
 // 8-bit floats: the products of a block of 128 k values are one instruction, whose four results per lane are added to the sums
-// with their scales, SA of the lane's row times SB of the wavefront's columns, while the matrix core works on the next.
+// with their scales, SA of the lane's row times SB of the wavefront's columns, while the matrix core works on the next.  Scales are
+// requested in R1, two steps ahead, in runs that share two places by turns (ragged_schedule.h).
 #include "common.h"
 #include "ragged.h"
+#include "ragged_schedule.h"
 #define ALIGNED 1
 #include "ragged_tile.h"
 
 constexpr int BM = 256, BN = 256, WJ = 4, NW = 8, THREADS = NW * 64, TM = 8, TN = 4, BK = 128 / ES;
 constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
 constexpr bool SCALED = IN_DT == DT_F8E4M3;
-constexpr int KB = 8, LS = KB * BM / 64 / NW; // k blocks whose scales are in LDS at a time, twice; loads of a wavefront for them
+constexpr int KB = SCALE_RUN, LS = KB * BM / 64 / NW; // k blocks whose scales are in LDS at a time, twice; loads of a wavefront for them
 constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, SB_BYTES = SCALED ? 256 : 0, OS = sizeof(out_t);
 constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, OUT_AT = SB_AT + 2 * SB_BYTES, TABLE_AT = OUT_AT + (OS == 2 ? NW * 1024 : 0);
 constexpr int LDS_BYTES = TABLE_AT + (WGRAD ? 2048 : GROUPED ? 4096 + 2048 : 0);
@@ -131,19 +133,21 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     const char *const a_ = g.a + inst * g.a_inst, *const b_ = g.b + inst * g.b_inst;
     const unsigned lds0 = lds_address(lds);
 
-    // ---- the cursor of the loads: step lk of `lsteps` of tile lt, the lf-th of the launch, into stage wr
+    // ---- the cursor of the loads: step lk of tile lt, the lf-th of the launch, into stage wr; a tile's steps are counted from `first` up to lsteps
     tile_t lt;
     unsigned lf = blockIdx.x;
-    int lk = 0, lsteps = 0, wr = 0, lchunk = 0; // lchunk: which of the two places the scales of its blocks go to
+    int lk = 0, lsteps = 0, wr = 0, lchunk = 0; // lchunk: which of the two places its run of scales goes to
     bool more = true;                           // false: past the last tile, the last step is requested again (never read)
     const char *la, *lb;                        // first row of the step's operands
     unsigned va[4], vb[4]; // of A's parts and B's halves two loads each, from la and lb
     const int chunk = lane % 8 ^ lane / 8;
     const int a_k = wave * 4 + lane / 16, b_k = wave * 2 + lane / 32; // k row of a transposed operand's load 0
 #if IN_DT == DT_F8E4M3
-    const int blocks = (g.depth + 127) / 128, col_blocks = (g.cols + 127) / 128;
+    const int blocks = (g.depth + 127) / 128, col_blocks = (g.cols + 127) / 128, first = first_step(blocks);
     unsigned vsa, vsb; // of the scales: row wave / 2 * 64 + lane; lane = 8 * (block of columns) + block of k
     static_assert(KB == 8 && LS == 4, "two wavefronts share 64 rows");
+#else
+    constexpr int first = 0; // no scales
 #endif
     // What is computed once for a tile stays there: hoisted out of the loops its parts would take the registers of the products.
     auto opaque = [](int x) {
@@ -162,8 +166,8 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
                 break;
             }
         }
-        lk = 0;
-        lsteps = (lt.depth + BK - 1) / BK;
+        lk = first;
+        lsteps = first + (lt.depth + BK - 1) / BK;
         la = scalar(a_ + (A_KC ? (long)lt.row * g.a_row : (long)lt.k0 * g.a_row + (long)lt.row * ES));
         lb = scalar(b_ + lt.expert * g.b_expert + (B_KC ? (long)lt.col * g.b_row : (long)lt.k0 * g.b_row + (long)lt.col * ES));
         const int cols = g.cols - lt.col;
@@ -193,7 +197,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     };
     // load l of step lk: 0, 1 of A0, 2 to 5 of B, 6, 7 of A1
     auto load = [&](int l, bool inner = false) { // inner: a step that the tile's reduction fills
-        const int here = lt.depth - lk * BK;
+        const int here = lt.depth - (lk - first) * BK;
         const bool of_a = l < 2 || l >= 6;
         const int n = l < 2 ? l : l >= 6 ? l - 4 : l - 2;
         unsigned v = of_a ? va[n] : vb[n];
@@ -206,17 +210,18 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         else at += A_BYTES + n * 8192;
         gather_lds16_at(buffer_at(of_a ? la : lb), v, 0, at);
     };
-    auto load_scales = [&]() {
+    auto load_scales = [&](bool inner = false) { // inner: not a tile's first step
 #if IN_DT == DT_F8E4M3
-        if (lk % KB == 0) {
+        if (inner ? lk % KB == 0 : starts_run(lk, first)) {
+            const int start = (inner ? lk : head_of_run(lk)) - first; // block at the head of the place: none ahead of block 0
             const char *const lsa = scalar((const char *)g.sa + inst * g.sa_inst + (long)lt.row * blocks * 4);
             const char *const lsb = scalar((const char *)g.sb + inst * g.sb_inst + ((long)lt.expert * col_blocks + lt.col / 128) * blocks * 4);
             // 64 rows of a wavefront, the blocks of one line after each other
             const int k0 = wave % 2 * LS;
             const unsigned at = lds0 + SC_AT + lchunk * SC_BYTES + (k0 * BM + wave / 2 * 64) * 4;
 #pragma unroll
-            for (int l = 0; l < LS; ++l) gather_lds4(buffer_at(lsa + (lk + k0 + l) * 4), lk + k0 + l < blocks ? vsa : OUTSIDE, at + l * BM * 4);
-            if (wave == 0) gather_lds4(buffer_at(lsb + lk * 4), lk + lane % KB < blocks ? vsb : OUTSIDE, lds0 + SB_AT + lchunk * SB_BYTES);
+            for (int l = 0; l < LS; ++l) gather_lds4(buffer_at(lsa + (start + k0 + l) * 4), (unsigned)(start + k0 + l) < (unsigned)blocks ? vsa : OUTSIDE, at + l * BM * 4);
+            if (wave == 0) gather_lds4(buffer_at(lsb + start * 4), (unsigned)(start + lane % KB) < (unsigned)blocks ? vsb : OUTSIDE, lds0 + SB_AT + lchunk * SB_BYTES);
         }
 #endif
     };
@@ -225,7 +230,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         ++lk;
         la += A_KC ? 128 : BK * g.a_row;
         lb += B_KC ? 128 : BK * g.b_row;
-        if (lk % KB == 0) lchunk ^= 1;
+        if (SCALED && lk % KB == 0) lchunk ^= 1;
     };
     auto advance = [&]() {
         if (more && lk + 1 < lsteps) {
@@ -414,8 +419,8 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     int rd = 0, cchunk = 0;
     zero();
     for (;;) {
-        const int steps = (ct.depth + BK - 1) / BK;
-        int k = 0;
+        const int steps = first + (ct.depth + BK - 1) / BK;
+        int k = first;
         auto step = [&](auto moves_on, bool inner) {
             if (SCALED && k && k % KB == 0) cchunk ^= 1;
             read_b(rd);
@@ -430,7 +435,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             barrier();
             read_a(rd, 1);
             read_scales(1, k, cchunk);
-            load_scales();
+            load_scales(inner);
             load(0, inner);
             load(1, inner);
             load(2, inner);

@@ -1518,7 +1518,7 @@ bool ms::layer_block_fits(const ms_op *op, int64_t code)
     const bool few = code % 1000 <= 32;
     if (!ragged_aligned(op)) return code == 64128;
     if (few) return ragged_by_k(op) && (code == 16016 || code == 16032 || code == 32032 || code == 64032);
-    if (code == 256256) return op->in_size == 2 || op->K > 128; // scales of a tile's blocks are overwritten two steps later
+    if (code == 256256) return op->in_size == 2 || op->K > 128; // a single block's scales would be a run of one step (ragged_schedule.h)
     return code == 64128 || code == 128128;
 }
 

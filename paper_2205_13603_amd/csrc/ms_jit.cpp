@@ -108,7 +108,7 @@ static int32_t get_source(const std::string &name, const Source **src) // entrie
     std::string marker = "#include \"common.h\"";
     size_t at = body.find(marker);
     if (at != std::string::npos) body.replace(at, marker.size(), common);
-    for (const char *header : {"ragged.h", "ragged_tile.h"}) { // of the products over rows by expert
+    for (const char *header : {"ragged.h", "ragged_tile.h", "ragged_schedule.h"}) { // of the products over rows by expert
         marker = std::string("#include \"") + header + "\"";
         at = body.find(marker);
         if (at == std::string::npos) continue;

@@ -203,3 +203,12 @@ def test_launches_on_several_threads_and_devices(tmp_path):
     env.pop("LD_PRELOAD", None)
     r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, env=env, timeout=600)
     assert r.returncode == 0 and "layer checks ok" in r.stdout, r.stdout[-6000:]
+
+
+def test_scales_of_whole_tiles_are_read_before_their_place_is_taken(tmp_path):
+    """The kernel's own arithmetic of the two places (ragged_schedule.h), walked phase by phase for 2 to 200 blocks of k."""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    exe = str(tmp_path / "ms_scales")
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-o", exe, os.path.join(root, "tests", "sanitize", "scales_driver.cpp")], check=True)
+    r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
+    assert r.returncode == 0 and "scales ok" in r.stdout, r.stdout
