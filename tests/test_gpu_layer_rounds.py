@@ -67,7 +67,8 @@ def test_scaled_product_of_several_whole_tiles_each(K, code):
     close(c, av @ bv.t(), av.abs() @ bv.abs().t(), K // 64 + 4, "bf16", f8=True)
 
 
-@pytest.mark.parametrize("kind,rows_of_k,K", [("f8", True, 272), ("f8", True, 1040), ("f8", True, 1152), ("f8", True, 2064)])
+@pytest.mark.parametrize("kind,rows_of_k,K", [("f8", True, 272), ("f8", True, 1040), ("f8", True, 1152), ("f8", True, 2064), ("bf16", True, 40), ("bf16", True, 72), ("f16", True, 192),
+                                              ("f16", False, 64), ("bf16", False, 328)])
 def test_grouped_product_of_several_whole_tiles_each(kind, rows_of_k, K):
     counts, ahead, behind, N = [1948, 0, 1950, 137, 250, 3], 2, 5, 8184
     E, T = len(counts), ahead + sum(counts) + behind
@@ -94,3 +95,20 @@ def test_grouped_product_of_several_whole_tiles_each(kind, rows_of_k, K):
         rows = slice(int(off[e]), int(off[e + 1]))
         if counts[e]:
             close(c[rows], av[rows] @ bv[e].t(), av[rows].abs() @ bv[e].abs().t(), K, out, f8=kind == "f8")
+
+
+def test_weight_gradient_of_several_whole_tiles_each():
+    """Tiles of unequal depths, from none and one step up, one after the other in a workgroup."""
+    counts, I, J = [700, 1, 0, 64, 65, 130, 3, 256, 0, 40], 2040, 2056
+    E, T = len(counts), sum(counts) + 3
+    v = variant(B.grouped_wgrad_op(E, T, I, J, "bf16", "bf16"), 256256)
+    if v is None:
+        return
+    assert E * 8 * 9 // torch.cuda.get_device_properties(0).multi_processor_count >= 2
+    _, normal = on_device(3)
+    p, q, off = normal(T, I).bfloat16(), normal(T, J).bfloat16(), offsets_of(counts, 1)
+    d = run_twice(v, [p, q, off.cuda()], torch.empty(E, I, J, dtype=torch.bfloat16, device="cuda"))
+    for e in range(E):
+        rows = slice(int(off[e]), int(off[e + 1]))
+        pv, qv = p[rows].double(), q[rows].double()
+        close(d[e], pv.t() @ qv, pv.abs().t() @ qv.abs(), max(1, counts[e]), "bf16")
