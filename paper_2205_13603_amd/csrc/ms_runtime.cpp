@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <atomic>
+#include <cinttypes>
 #include <cstring>
 #include <map>
 #include <mutex>
@@ -366,6 +367,8 @@ static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *cons
         void *s = d.out_dtype == MS_F8E4M3 ? outputs[1] : nullptr, *h = d.has_bias ? outputs[2] : nullptr;
         if (!aligned(x, op.in_size) || !aligned(w, op.in_size) || !aligned(res, op.in_size) || !aligned(h, op.in_size) || !aligned(outputs[0], op.out_size) || !aligned(s, 4))
             return fail(MS_ERR_BAD_ARG, "ms_variant_launch: a tensor is not aligned to its elements");
+        if (h && h == x && op.M > 1 && d.a_strides[1] != op.K) // rows of H would be written over rows of X that are still to be read
+            return fail(MS_ERR_BAD_ARG, "ms_variant_launch: H has dense rows and cannot be X, whose rows are %" PRId64 " elements apart", d.a_strides[1]);
         r = {x, w, res, outputs[0], s, h, d.a_strides[1], (op.M - 1) * d.a_strides[1] + op.K, (int32_t)op.M, (int32_t)op.K, instances, (float)((double)d.dims[2] * MS_EPS_UNIT)};
         const int64_t groups = (op.M * instances + v->p.block_m - 1) / v->p.block_m;
         gx = (unsigned)std::min<int64_t>(groups, 1 << 20); // workgroups go on to further rows

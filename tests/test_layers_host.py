@@ -6,7 +6,7 @@ import subprocess
 import numpy as np
 import pytest
 
-from paper_2205_13603_amd import binding as B
+from paper_2205_13603_amd import binding as B, devmem
 
 OPS = {
     "norm": lambda: B.rms_norm_op(37, 1000, "bf16", "f8"),
@@ -212,3 +212,20 @@ def test_scales_of_whole_tiles_are_read_before_their_place_is_taken(tmp_path):
     subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-o", exe, os.path.join(root, "tests", "sanitize", "scales_driver.cpp")], check=True)
     r = subprocess.run([exe], stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True, timeout=60)
     assert r.returncode == 0 and "scales ok" in r.stdout, r.stdout
+
+
+def test_the_sum_is_not_written_over_rows_further_apart():
+    """H is dense: over an X of longer rows it would cover rows that other workgroups have yet to read.  What is allowed gets as far as the GPU's
+    runtime, which is not there."""
+    def norm(M, **kw):
+        op = B.rms_norm_op(M, 16, "bf16", **kw)
+        space = op.space()
+        return B.Variant(op, space, B.default_trace(space))
+
+    x, w, r, y = ((1 + i) << 20 for i in range(4))
+    wide = dict(a_strides=[0, 24, 1])
+    refused(B.MS_ERR_BAD_ARG, norm(4, **wide).launch, [x, w, r], [y, None, x])
+    refused(B.MS_ERR_BAD_ARG, norm(4, **wide).launch, [x, w, r], [y, None, x], instances=2)
+    if not devmem.gpu_available():
+        for v, h in ((norm(4), x), (norm(4, a_strides=[0, 16, 1]), x), (norm(4, **wide), r), (norm(1, **wide), x)):
+            refused(B.MS_ERR_HIP, v.launch, [x, w, r], [y, None, h])
