@@ -81,6 +81,21 @@ __device__ __forceinline__ unsigned max16(unsigned x)
     o = across<0x140>(x);
     return x > o ? x : o;
 }
+// y / s in fp32 as close as the rounding to 8-bit floats can tell from a division's: the reciprocal in two parts is within 3 * 2^-48 of itself, which
+// leaves a quotient on its side of every tie and on the ties themselves.  (Only 518 pairs of significands have quotients so near to where the fp32
+// rounding would cross one; all of them come out as the division's.  The rounded reciprocal alone, 1.5 units off, moves one near tie in four.  16384 x 8192 in
+// bf16: 171.6 us with the reciprocal, 174.4 this way, 181 with divisions.)
+__device__ __forceinline__ void quotients(float (&y)[8], float s)
+{
+    if (s > 0x1p60f) { // the second part would be subnormal
+        s *= 0x1p-60f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] *= 0x1p-60f;
+    }
+    const float to = 1.f / s, rest = s < __builtin_inff() ? __builtin_fmaf(-s, to, 1.f) * to : 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y[i] = __builtin_fmaf(y[i], to, y[i] * rest);
+}
 __device__ __forceinline__ float lane_of(float x, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), lane)); }
 
 extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rms_args g)
@@ -152,12 +167,12 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rms_args g
                 float s = __uint_as_float(max16(most)) / LARGEST;
                 s = s < LEAST ? LEAST : s; // NaN stays
                 if (lane % 16 == 0) g.s[row * blocks + c / 128] = s;
-                const float to = 1.f / s;
+                quotients(y, s);
                 int lo = 0, hi = 0;
-                lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0] * to, y[1] * to, lo, false);
-                lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2] * to, y[3] * to, lo, true);
-                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4] * to, y[5] * to, hi, false);
-                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6] * to, y[7] * to, hi, true);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], lo, false);
+                lo = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], lo, true);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[4], y[5], hi, false);
+                hi = __builtin_amdgcn_cvt_pk_fp8_f32(y[6], y[7], hi, true);
                 char *o = (char *)g.y + at + c;
                 if (n >= 8) {
                     __builtin_nontemporal_store(u2a_t{(unsigned)lo, (unsigned)hi}, reinterpret_cast<u2a_t *>(o));

@@ -671,3 +671,34 @@ def test_measure_and_search():
     torch.cuda.synchronize()
     for at, t in zip(places, (y, s, h)):
         assert torch.equal(out[at:at + t.numel()], t)
+
+
+def test_rms_norm_divides_by_its_scales():
+    """Rows of ones have a norm of one, so that Y is W in 8-bit floats: values at and next to the ties of each block's scale, of all magnitudes,
+    come out as the fp32 quotient W / S rounds."""
+    blocks = 4096
+    N = blocks * 128
+    v = variant(B.rms_norm_op(1, N, "f32", "f8", residual=False, eps=0))
+    if v is None:
+        return
+    g = rng(77)
+    most = 448 * torch.ldexp(1 + torch.rand(blocks, generator=g), torch.randint(-132, 116, (blocks,), generator=g))
+    most[:256] = 448 * torch.ldexp(torch.tensor(1.0), torch.randint(-126, 116, (256,), generator=g))  # powers of two
+    s = (most / 448).clamp_min(2.0 ** -126)
+    normal_ties = torch.ldexp((torch.randint(8, 16, (blocks, 64), generator=g) * 2 + 1).float(), torch.randint(-10, 5, (blocks, 64), generator=g))
+    subnormal_ties = (torch.randint(0, 8, (blocks, 63), generator=g) * 2 + 1) * 2.0 ** -10
+    w = torch.cat([normal_ties, subnormal_ties], 1).clamp(max=440) * s[:, None]
+    w = (w.view(torch.int32) + torch.randint(-3, 4, w.shape, generator=g, dtype=torch.int32)).clamp_min(0).view(torch.float32)
+    w = torch.cat([torch.minimum(w, most[:, None]), most[:, None]], 1)
+    w[-1, 5] = float("inf")  # its scale too: finite values become 0, the infinity NaN
+    s = (w.amax(1) / 448).clamp_min(2.0 ** -126)
+    w = w * (torch.randint(0, 2, w.shape, generator=g) * 2 - 1)
+    want = (w / s[:, None]).to(TYPES["f8"])
+    assert int(((w * (1 / s)[:, None]).to(TYPES["f8"]).view(torch.uint8) != want.view(torch.uint8)).sum()) > 10000  # a reciprocal does not do
+    y, got, _ = launch_twice(v, [dev(torch.ones(1, N)), dev(w.reshape(-1)), None], [((1, N), TYPES["f8"]), ((1, blocks), torch.float32), None])
+    assert torch.equal(got[0], s)
+    y = y.view(blocks, 128)
+    nan = torch.isnan(want.float())
+    assert torch.equal(torch.isnan(y.float()), nan) and int(nan.sum()) == 1
+    off = (y.view(torch.uint8) != want.view(torch.uint8)) & ~nan
+    assert not bool(off.any()), "%d values off, the first %r / %r" % (int(off.sum()), float(w[off][0]), float(s[off.nonzero()[0, 0]]))
