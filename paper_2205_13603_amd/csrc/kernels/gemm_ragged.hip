@@ -33,7 +33,7 @@ extern "C" __global__ void __launch_bounds__(tile::THREADS) ms_kernel(const ragg
     } else {
         // products deal runs of tiles to the XCDs, so that the workgroups that run together on one XCD share rows and columns in its L2
         const unsigned total = tiles_of<tile::BM, tile::BN>(g, table);
-        if (blockIdx.x >= total || !decode<tile::BM, tile::BN>(g, offsets, table, WGRAD ? blockIdx.x : xcd_run<0>(blockIdx.x, total), lane, t)) return;
+        if (blockIdx.x >= total || !decode<tile::BM, tile::BN>(g, offsets, table, WGRAD ? blockIdx.x : run_of_xcd(blockIdx.x, total), lane, t)) return;
     }
     tile::make(g, inst, t, lds);
 }

@@ -22,7 +22,6 @@
 // requested in R1, two steps ahead, in runs that share two places by turns (ragged_schedule.h).
 #include "common.h"
 #include "ragged.h"
-#include "ragged_schedule.h"
 #define ALIGNED 1
 #include "ragged_tile.h"
 
@@ -35,7 +34,6 @@ constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, OUT_AT = SB_AT + 
 constexpr int LDS_BYTES = TABLE_AT + (WGRAD ? 2048 : GROUPED ? 4096 + 2048 : 0);
 typedef ragged_tile<128, 128, 2, 2, 2> quarter;
 static_assert(quarter::LDS_BYTES <= TABLE_AT, "quarters lie where whole tiles did");
-constexpr unsigned QUARTER = 40; // time of a quarter in hundredths of a whole tile's (8 bits, 4096 deep: 26.6 us of 68; bf16: 42 of 105)
 static_assert(LDS_BYTES == LDS_HOST, "the host's count of LDS");
 
 extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_args g)
@@ -52,7 +50,8 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     // ---- the tiles.  Products: whole ones, of up to 256 rows but more than 128, then quarters of 128 x 128: the rest of each expert's rows,
     // and the whole tiles of a last round that would leave most workgroups without one.
     const unsigned nt = (unsigned)(g.cols + BN - 1) / BN;
-    unsigned total, half_rows = 0, quarters = 0;
+    unsigned total, half_rows = 0;
+    rounds_t rounds = {0, 0};
     if constexpr (WGRAD) {
         // experts by their rows, most first, and every other round backwards: the workgroups' sums of rows are then nearly the same
         int *rows = reinterpret_cast<int *>(lds);
@@ -76,51 +75,43 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             full_rows = table[g.experts - 1];
             half_rows = uniform((unsigned)halves[g.experts - 1]);
         } else {
-            full_rows = (g.rows + 127) / 256;
-            half_rows = g.rows > full_rows * 256;
+            full_rows = whole_tiles(g.rows);
+            half_rows = half_left(g.rows);
         }
-        total = uniform((unsigned)full_rows) * nt;
-        const unsigned rest = total % gridDim.x, of_halves = half_rows * nt * 2;
-        auto rounds = [&](unsigned n) { return (n + gridDim.x - 1) / gridDim.x; };
-        if (rest && rounds(4 * rest + of_halves) * QUARTER < 100 + rounds(of_halves) * QUARTER) {
-            total -= rest;
-            quarters = 4 * rest;
-        }
-        quarters += of_halves;
+        rounds = split_rounds(uniform((unsigned)full_rows) * nt, half_rows * nt, gridDim.x);
+        total = rounds.whole;
     }
     // the tile of a workgroup's f-th turn, f counted in steps of the grid; false: there is nothing to do
     auto tile_of = [&](unsigned f, tile_t &t) {
         if (WGRAD) {
-            const unsigned round = f / gridDim.x;
-            if (round & 1) f = round * gridDim.x + (gridDim.x - 1 - (f - round * gridDim.x));
+            f = back_and_forth(f, gridDim.x);
             return f < total && decode<BM, BN>(g, offsets, table, f, lane, t, order);
         }
-        return decode<BM, BN, true>(g, offsets, table, xcd_run<0>(f, total), lane, t);
+        return decode<BM, BN, true>(g, offsets, table, run_of_xcd(f, total), lane, t);
     };
     const unsigned turns = WGRAD ? (total + gridDim.x - 1) / gridDim.x * gridDim.x : total;
     auto make_quarters = [&]() {
         if constexpr (!WGRAD) {
-            for (unsigned f = blockIdx.x; f < quarters; f += gridDim.x) {
-                const unsigned q = xcd_run<0>(f, quarters), of_whole = quarters - half_rows * nt * 2;
+            for (unsigned f = blockIdx.x; f < rounds.quarters; f += gridDim.x) {
+                const quarter_t q = quarter_of(run_of_xcd(f, rounds.quarters), rounds, half_rows * nt, nt);
                 tile_t t;
                 bool any;
-                if (q < of_whole) {
-                    any = decode<BM, BN, true>(g, offsets, table, total + q / 4, lane, t);
-                    t.row += q % 2 * 128;
-                    t.rows -= q % 2 * 128;
-                    t.col += q % 4 / 2 * 128;
+                if (!q.half) {
+                    any = decode<BM, BN, true>(g, offsets, table, q.tile, lane, t);
+                    t.row += q.row;
+                    t.rows -= q.row;
+                    t.col += q.col;
                 } else {
-                    const unsigned h = q - of_whole, row = h / (nt * 2);
                     tile_at where = {0, 0, 1};
-                    int first = 0, end = g.rows, whole = (g.rows + 127) / 256;
+                    int first = 0, end = g.rows;
                     if (GROUPED) {
-                        where = find_tile(halves, g.experts, (int)row, lane);
+                        where = find_tile(halves, g.experts, (int)q.tile, lane);
                         const range_t r = rows_of(offsets, where.expert, g.rows);
                         first = __builtin_amdgcn_readfirstlane(r.first);
                         end = __builtin_amdgcn_readfirstlane(r.last);
-                        whole = (end - first + 127) / 256;
                     }
-                    t = {where.expert, first + whole * 256, end - first - whole * 256, (int)(h % (nt * 2)) * 128, 0, g.depth};
+                    const int whole = whole_tiles(end - first) * 256;
+                    t = {where.expert, first + whole, end - first - whole, (int)q.col, 0, g.depth};
                     any = true;
                 }
                 t.rows = t.rows < 128 ? t.rows : 128;

@@ -36,7 +36,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             if (!find_row_tile(g.offsets + (long)inst * (g.experts + 1), g.experts, g.rows, BM, nt, blockIdx.x, lane, wave, table, where, of, r)) return;
             expert = where.expert;
         } else {
-            of = xcd_run<0>(blockIdx.x, (unsigned)where.tiles * nt);
+            of = run_of_xcd(blockIdx.x, (unsigned)where.tiles * nt);
         }
         row = r.first + of % (unsigned)where.tiles * BM;
         col = of / (unsigned)where.tiles * BN;

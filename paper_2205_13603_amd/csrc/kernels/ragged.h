@@ -1,4 +1,5 @@
 // Shared by the kernels of products over rows that lie sorted by expert.
+#include "ragged_schedule.h"
 
 // As RaggedArgs in ms_internal.h: distances in bytes.  depth, cols and rows of a gradient of weights are T, J and I.
 struct ragged_args {
@@ -97,8 +98,8 @@ __device__ __forceinline__ void count_wide_tiles(const int *offsets, int experts
         int n = 0, h = 0;
         if (e < experts) {
             const range_t r = rows_of(offsets, e, total);
-            n = (r.last - r.first + 127) / 256;
-            h = r.last - r.first > n * 256;
+            n = whole_tiles(r.last - r.first);
+            h = half_left(r.last - r.first);
         }
         const unsigned long m = __ballot(h); // halves of the lanes up to this one
         h = before_h + __builtin_popcountl(m & (~0ul >> (63 - lane)));
@@ -140,7 +141,7 @@ __device__ __forceinline__ bool find_row_tile(const int *offsets, int experts, i
         if (lane < experts) r = rows_of(offsets, lane, total);
         const int n = sums_of_lanes((r.last - r.first + bm - 1) / bm), all = __builtin_amdgcn_readlane(n, 63);
         if (block >= (unsigned)all * nt) return false;
-        const unsigned f = xcd_run<0>(block, (unsigned)all * nt);
+        const unsigned f = run_of_xcd(block, (unsigned)all * nt);
         const int t = uniform(f / nt), e = __builtin_ctzl(__ballot(n > t));
         const int from = e ? __builtin_amdgcn_readlane(n, e - 1) : 0, to = __builtin_amdgcn_readlane(n, e);
         where = {e, t - from, to - from};
@@ -152,7 +153,7 @@ __device__ __forceinline__ bool find_row_tile(const int *offsets, int experts, i
     barrier();
     const unsigned all = uniform((unsigned)table[experts - 1]) * nt;
     if (block >= all) return false;
-    const unsigned f = xcd_run<0>(block, all);
+    const unsigned f = run_of_xcd(block, all);
     where = find_tile(table, experts, (int)(f / nt), lane);
     if ((unsigned)where.tile >= (unsigned)where.tiles) return false; // offsets that decrease: nothing outside the tensors is touched
     of = f - (unsigned)(f / nt - where.tile) * nt;
@@ -175,15 +176,13 @@ template <int TR, int TC> __device__ __forceinline__ unsigned tiles_of(const rag
     return (unsigned)((g.rows + TR - 1) / TR) * nt * (WGRAD ? (unsigned)g.experts : 1u);
 }
 
-// The `of`-th tile of an expert (or of the one matrix) with row tiles `where` and rows `r`: 8 row tiles by all columns at a time, rows first.
-// false: it has no rows.
+// The `of`-th tile of an expert (or of the one matrix) with row tiles `where` and rows `r`.  false: it has no rows.
 template <int TR, int TC> __device__ __forceinline__ bool tile_from(const ragged_args &g, const tile_at &where, unsigned of, unsigned nt, const range_t &r, tile_t &t)
 {
-    constexpr unsigned GM = 8;
-    const unsigned band = of / (GM * nt), in = of - band * GM * nt, rest = (unsigned)where.tiles - band * GM, high = rest < GM ? rest : GM;
+    const tile_in_bands at = in_bands(of, (unsigned)where.tiles, nt);
     t.expert = where.expert;
-    t.col = (int)(in / high) * TC;
-    t.row = (int)(band * GM + in % high) * TR;
+    t.col = (int)at.col * TC;
+    t.row = (int)at.row * TR;
     t.k0 = 0;
     t.depth = g.depth;
     int end = g.rows;
@@ -211,11 +210,11 @@ template <int TR, int TC, bool WIDE = false> __device__ __forceinline__ bool dec
     tile_at where;
     unsigned of;
     if (WGRAD || !GROUPED) {
-        const int mt = WIDE ? (g.rows + 127) / 256 : (g.rows + TR - 1) / TR;
+        const int mt = WIDE ? whole_tiles(g.rows) : (g.rows + TR - 1) / TR;
         const unsigned each = (unsigned)mt * nt;
         where = {(int)(f / each), 0, mt};
         of = f % each;
-        if (WGRAD && each % 8 == 0) of = xcd_run<0>(of, each); // an expert's tiles over all XCDs: experts differ in their rows
+        if (WGRAD && each % 8 == 0) of = run_of_xcd(of, each); // an expert's tiles over all XCDs: experts differ in their rows
         if (order) where.expert = order[where.expert];
     } else {
         where = find_tile(table, g.experts, (int)(f / nt), lane);

@@ -3,6 +3,7 @@
 // schedule of Table 2, applied in a fixed order per kernel family), plus the
 // hardware-limit checks of the paper's "Trace validation" paragraph.
 // Host only.
+#include "kernels/ragged_schedule.h"
 #include "ms_internal.h"
 
 #include <algorithm>
@@ -1826,6 +1827,105 @@ static inline int64_t split_index(const int32_t *f, int64_t x0, int64_t x1, int6
     return ((x0 * f[1] + x1) * f[2] + x2) * f[3] + x3;
 }
 
+// ---- walks of the kernels of layers: their workgroups, wavefronts and lanes
+
+// Columns of the chunks of 8 that the lanes of a row's wavefronts take.
+template <class F> static void rms_columns(const ms_op *op, const ms_variant_params *p, F column)
+{
+    const int64_t step = (int64_t)p->body_tile * 512;
+    for (int64_t c0 = 0; c0 < step; c0 += 8)
+        for (int64_t c = c0; c < op->K; c += step)
+            for (int64_t i = c; i < std::min(op->K, c + 8); ++i) column(i);
+}
+
+static void rms_coverage(const ms_op *op, const ms_variant_params *p, int32_t *counts)
+{
+    const int64_t groups = p->threads / 64 / p->body_tile, workgroups = std::min<int64_t>(p->grid[0], 1 << 20);
+    for (int64_t b = 0; b < workgroups; ++b)
+        for (int64_t base = b * groups; base < op->M; base += workgroups * groups)
+            for (int64_t row = base; row < std::min(op->M, base + groups); ++row) rms_columns(op, p, [&](int64_t c) { ++counts[row * op->K + c]; });
+}
+
+// What the wavefronts of a workgroup store of the tile at (row, col): its rows from there up to `end`, its columns up to the last.
+static void ragged_tile_coverage(const ms_op *op, const RaggedTile &t, int64_t expert, int64_t row, int64_t end, int64_t col, int32_t *counts)
+{
+    auto block = [&](int64_t i, int64_t j) { // 16 x 16 results from row i and column j of the tile
+        for (int64_t r = row + i; r < std::min(end, row + i + 16); ++r)
+            for (int64_t c = col + j; c < std::min(op->N, col + j + 16); ++c) ++counts[(expert * op->M + r) * op->N + c];
+    };
+    if (t.few) {
+        const int waves = t.wi, tiles = t.bm / 16 * (t.bn / 16);
+        for (int w = 0; w < waves; ++w)
+            for (int n = w; n < tiles; n += waves) block(n / (t.bn / 16) * 16, n % (t.bn / 16) * 16);
+        return;
+    }
+    const int tm = t.bm / t.wi / 16, tn = t.bn / t.wj / 16, half = tm / t.groups;
+    for (int g = 0; g < t.groups; ++g)
+        for (int i = 0; i < t.wi; ++i)
+            for (int j = 0; j < t.wj; ++j)
+                for (int a = 0; a < half; ++a)
+                    for (int b = 0; b < tn; ++b) block((i * tm + g * half + a) * 16, (j * tn + b) * 16);
+}
+
+// Every workgroup's tiles; of a grouped product all rows are taken for one expert's.
+static void ragged_coverage(const ms_op *op, const ms_variant_params *p, int32_t *counts)
+{
+    const RaggedTile t = ragged_tile(op, p->body_tile);
+    const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD;
+    const unsigned nt = (unsigned)((op->N + t.bn - 1) / t.bn), mt = (unsigned)((op->M + t.bm - 1) / t.bm), experts = wgrad ? (unsigned)op->nb : 1;
+    auto place = [&](int64_t expert, unsigned of, unsigned tiles) {
+        const tile_in_bands at = in_bands(of, tiles, nt);
+        ragged_tile_coverage(op, t, expert, (int64_t)at.row * t.bm, op->M, (int64_t)at.col * t.bn, counts);
+    };
+    auto of_gradient = [&](unsigned f) { // an expert's tiles over all XCDs
+        const unsigned each = mt * nt, of = f % each;
+        place(f / each, each % 8 == 0 ? run_of_xcd(of, each) : of, mt);
+    };
+    if (p->body != MS_BODY_RAGGED_PHASES) { // a tile for each workgroup
+        const unsigned total = mt * nt * experts;
+        for (unsigned b = 0; b < std::min((unsigned)p->grid[0], total); ++b) {
+            const unsigned f = wgrad ? b : run_of_xcd(b, total);
+            if (t.few) ragged_tile_coverage(op, t, 0, (int64_t)(f % mt) * t.bm, op->M, (int64_t)(f / mt) * t.bn, counts);
+            else if (wgrad) of_gradient(f);
+            else place(0, f, mt);
+        }
+        return;
+    }
+    const unsigned grid = std::min(4u * (unsigned)p->grid[0], 256u); // workgroups on a card of 256 compute units
+    if (wgrad) { // experts in any order
+        const unsigned total = mt * nt * experts, turns = (total + grid - 1) / grid * grid;
+        for (unsigned b = 0; b < grid; ++b)
+            for (unsigned f = b; f < turns; f += grid) {
+                const unsigned turn = back_and_forth(f, grid);
+                if (turn < total) of_gradient(turn);
+            }
+        return;
+    }
+    const unsigned whole = (unsigned)whole_tiles((int)op->M), halves = half_left((int)op->M) ? nt : 0;
+    const rounds_t rounds = split_rounds(whole * nt, halves, grid);
+    RaggedTile quarter = t;
+    quarter.bm = quarter.bn = 128;
+    quarter.wi = quarter.wj = quarter.groups = 2;
+    for (unsigned b = 0; b < grid; ++b) {
+        for (unsigned f = b; f < rounds.whole; f += grid) place(0, run_of_xcd(f, rounds.whole), whole);
+        for (unsigned f = b; f < rounds.quarters; f += grid) {
+            const quarter_t q = quarter_of(run_of_xcd(f, rounds.quarters), rounds, halves, nt);
+            const tile_in_bands at = q.half ? tile_in_bands{whole, 0} : in_bands(q.tile, whole, nt);
+            ragged_tile_coverage(op, quarter, 0, (int64_t)at.row * 256 + q.row, op->M, (int64_t)at.col * 256 + q.col, counts);
+        }
+    }
+}
+
+// k values of a tile's sums, of an expert with all rows: steps of block_k, shared by the wavefronts (few rows) or taken by their groups in turn.
+static void ragged_reduction(const ms_op *op, const ms_variant_params *p, int32_t *counts)
+{
+    const RaggedTile t = ragged_tile(op, p->body_tile);
+    const int64_t bk = p->block_k, steps = (op->K + bk - 1) / bk, sharers = t.few ? t.wi : t.groups;
+    for (int64_t s = 0; s < sharers; ++s)
+        for (int64_t n = s; n < steps; n += sharers)
+            for (int64_t k = n * bk; k < std::min(op->K, n * bk + bk); ++k) ++counts[k];
+}
+
 extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params *p, int32_t *counts, int64_t out_elems)
 {
     if (!op || !p || !counts) return fail(MS_ERR_BAD_ARG, "ms_variant_coverage: NULL argument");
@@ -1835,13 +1935,8 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
     memset(counts, 0, sizeof(int32_t) * (size_t)out_elems);
     const ms_op_desc &d = op->d;
     if (is_layer_family(p->family)) {
-        // rows and columns behind the last are masked; of a grouped product all rows taken for one expert's
-        const int64_t rows = op->M, cols = d.kind == MS_OP_RMS_NORM ? op->K : op->N, bn = d.kind == MS_OP_RMS_NORM ? cols : p->block_n;
-        for (int64_t e = 0; e < (d.kind == MS_OP_GROUPED_WGRAD ? op->nb : 1); ++e)
-            for (int64_t i0 = 0; i0 < rows; i0 += p->block_m)
-                for (int64_t j0 = 0; j0 < cols; j0 += bn)
-                    for (int64_t i = i0; i < std::min(rows, i0 + p->block_m); ++i)
-                        for (int64_t j = j0; j < std::min(cols, j0 + bn); ++j) ++counts[(e * rows + i) * cols + j];
+        if (p->family == MS_FAM_RMS_NORM) rms_coverage(op, p, counts);
+        else ragged_coverage(op, p, counts);
         return MS_OK;
     }
     if (p->body == MS_BODY_IMAGE_ROWS) {
@@ -1966,13 +2061,13 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
 extern "C" int32_t ms_variant_reduction_coverage(const ms_op *op, const ms_variant_params *p, int32_t *counts, int64_t k_elems, int64_t *needed)
 {
     if (!op || !p) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
-    if (is_layer_family(p->family)) { // steps of block_k from the first k on, masked behind the last
+    if (is_layer_family(p->family)) {
         if (needed) *needed = op->K;
         if (!counts) return needed ? MS_OK : fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
         if (k_elems != op->K) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: k_elems %" PRId64 " != %" PRId64, k_elems, op->K);
         memset(counts, 0, sizeof(int32_t) * (size_t)k_elems);
-        for (int64_t k0 = 0; k0 < op->K; k0 += p->block_k)
-            for (int64_t k = k0; k < std::min(op->K, k0 + p->block_k); ++k) ++counts[k];
+        if (p->family == MS_FAM_RMS_NORM) rms_columns(op, p, [&](int64_t k) { ++counts[k]; });
+        else ragged_reduction(op, p, counts);
         return MS_OK;
     }
     const bool dw = p->family == MS_FAM_DWCONV;

@@ -229,3 +229,37 @@ def test_the_sum_is_not_written_over_rows_further_apart():
     if not devmem.gpu_available():
         for v, h in ((norm(4), x), (norm(4, a_strides=[0, 16, 1]), x), (norm(4, **wide), r), (norm(1, **wide), x)):
             refused(B.MS_ERR_HIP, v.launch, [x, w, r], [y, None, h])
+
+
+@pytest.mark.parametrize("make,code", [
+    (lambda: B.scaled_gemm_op(300, 500, 256), 16032), (lambda: B.scaled_gemm_op(300, 500, 256), 64128), (lambda: B.grouped_gemm_op(1, 700, 1500, 64), 128128),
+    (lambda: B.grouped_wgrad_op(3, 90, 136, 200), 64128)])
+def test_coverage_is_that_of_the_workgroups_there_are(make, code):
+    """One workgroup fewer than the launch has leaves its tile without a visit."""
+    op = make()
+    space = op.space()
+    p = B.trace_validate(op, space, B.make_trace(space, [[code]]))
+    d = op.desc()
+    n = op.tensor_bytes(-1) // {B.F32: 4, B.F16: 2, B.BF16: 2}[d.out_dtype]
+    assert (B.variant_coverage(op, p, n) == 1).all()
+    p.grid[0] -= 1
+    counts = B.variant_coverage(op, p, n)
+    assert counts.max() == 1 and 0 < (counts == 0).sum() <= p.block_m * p.block_n
+
+
+@pytest.mark.parametrize("M,N,K", [(2900, 6000, 400), (2816, 9176, 272), (8492, 4104, 144), (100, 70, 256), (129, 70, 256), (128 * 7, 257, 256), (256 * 16 + 1, 256 * 16 - 3, 256),
+                                   (256 * 33, 256 * 9, 144)])
+def test_whole_tiles_halves_and_quarters_cover_each_result_once(M, N, K):
+    op = B.scaled_gemm_op(M, N, K)
+    space = op.space()
+    p = B.trace_validate(op, space, B.make_trace(space, [[256256]]))
+    assert (B.variant_coverage(op, p, M * N) == 1).all()
+
+
+def test_tiles_of_gradients_cover_each_result_once():
+    for E, I, J in ((24, 1032, 520), (3, 2048, 2048), (700, 24, 40), (1, 304, 4000)):
+        op = B.grouped_wgrad_op(E, 100, I, J)
+        space = op.space()
+        for code in (64128, 128128, 256256):
+            p = B.trace_validate(op, space, B.make_trace(space, [[code]]))
+            assert (B.variant_coverage(op, p, E * I * J) == 1).all()
