@@ -437,9 +437,11 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             rd ^= 1;
             ++k;
         };
+        // the cursor of a tile of one step is in the next tile from the start, which is as deep (products) or need not be (gradients)
+        const bool reaches = !WGRAD || steps > 1;
         // the last steps, in which the cursor goes on to the next tile, in a loop of their own: its registers are not the others'
 #pragma unroll 1
-        while (more && lk + 2 < lsteps) step(next_step, true); // requests of steps lk and lk + 1, neither the tile's last
+        while (reaches && more && lk + 2 < lsteps) step(next_step, true); // requests of steps lk and lk + 1, neither the tile's last
 #pragma unroll 1
         while (k < steps) step(advance, false);
         store(ct);
