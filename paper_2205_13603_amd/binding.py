@@ -359,10 +359,14 @@ def norm_op(B, M, N, in_dtype="f32"):
 # ---- layers of language models (ms_op_desc has their definitions)
 def rms_norm_op(M, N, in_dtype="bf16", out_dtype=None, residual=True, eps=1e-6, **kw):
     """RMS norm of rows; inputs (X [M, N], W [N], R [M, N] with a residual), outputs (Y [M, N], S, H): S fp32 [M, ceil(N / 128)] for
-    out_dtype "f8", H = X + R [M, N] with a residual, None where there is none."""
+    out_dtype "f8", H = X + R [M, N] with a residual, None where there is none.  eps is held in units of EPS_UNIT; one that this would change by
+    more than a thousandth is refused."""
     if not 0 <= eps <= 1:
         raise ValueError("eps = %r" % (eps,))
-    return Op(OP_RMS_NORM, in_dtype, out_dtype or in_dtype, [M, N, round(eps / EPS_UNIT)], has_bias=residual, **kw)
+    units = round(eps / EPS_UNIT)
+    if abs(units * EPS_UNIT - eps) > eps / 1000:
+        raise ValueError("eps = %r is no multiple of %g" % (eps, EPS_UNIT))
+    return Op(OP_RMS_NORM, in_dtype, out_dtype or in_dtype, [M, N, units], has_bias=residual, **kw)
 
 
 def scaled_gemm_op(M, N, K, out_dtype="bf16", **kw):

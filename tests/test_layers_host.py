@@ -263,3 +263,11 @@ def test_tiles_of_gradients_cover_each_result_once():
         for code in (64128, 128128, 256256):
             p = B.trace_validate(op, space, B.make_trace(space, [[code]]))
             assert (B.variant_coverage(op, p, E * I * J) == 1).all()
+
+
+def test_an_eps_between_units_is_refused():
+    for eps in (1e-13, 4e-13, 5e-13, 1.5e-12, 2.45e-11):
+        with pytest.raises(ValueError):
+            B.rms_norm_op(4, 16, eps=eps)
+    for eps, units in ((0, 0), (1e-12, 1), (1e-6, 10 ** 6), (float(np.float32(1e-5)), 10 ** 7), (1.2345e-8, 12345), (1, 10 ** 12)):
+        assert B.rms_norm_op(4, 16, eps=eps).desc().dims[2] == units
