@@ -199,7 +199,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         unsigned at = lds0 + wr * STAGE + wave * 1024;
         if (of_a) at += A_KC ? n % 2 * 16384 + n / 2 * 8192 : n / 2 * 16384 + n % 2 * 8192;
         else at += A_BYTES + n * 8192;
-        gather_lds16_at(buffer_at(of_a ? la : lb), v, 0, at);
+        gather_lds16_at(buffer_at(of_a ? la : lb), v, at);
     };
     auto load_scales = [&](bool inner = false) { // inner: not a tile's first step
 #if IN_DT == DT_F8E4M3

@@ -67,9 +67,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         const unsigned at = ring + stage * SLOT;
         const bool tail = here < 128;
 #pragma unroll
-        for (int l = 0; l < LB; ++l) gather_lds16_at(rb, tail && chunk * 16 >= here ? OUTSIDE : bvoff[l], 0, at + BM * 128 + l * 1024);
+        for (int l = 0; l < LB; ++l) gather_lds16_at(rb, tail && chunk * 16 >= here ? OUTSIDE : bvoff[l], at + BM * 128 + l * 1024);
 #pragma unroll
-        for (int l = 0; l < LA; ++l) gather_lds16_at(ra, tail && chunk * 16 >= here ? OUTSIDE : avoff[l], 0, at + l * 1024);
+        for (int l = 0; l < LA; ++l) gather_lds16_at(ra, tail && chunk * 16 >= here ? OUTSIDE : avoff[l], at + l * 1024);
 #if IN_DT == DT_F8E4M3
         gather_lds4(sa, lane < rows ? (unsigned)(lane * blocks + k) * 4 : OUTSIDE, at + (BM + BN) * 128);
         gather_lds4(sb, lane == 0 ? (unsigned)k * 4 : OUTSIDE, at + (BM + BN) * 128 + 256);

@@ -232,10 +232,9 @@ __device__ __forceinline__ void gather_lds4(const rsrc_t &buffer, unsigned voff,
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dword %1, %2, 0 offen lds" : : "s"(uniform(dst)), "v"(voff), "s"(buffer) : "memory", "m0");
 }
-__device__ __forceinline__ void gather_lds16_at(const rsrc_t &buffer, unsigned voff, unsigned soff, unsigned dst)
+__device__ __forceinline__ void gather_lds16_at(const rsrc_t &buffer, unsigned voff, unsigned dst)
 {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds"
-                 : : "s"(uniform(dst)), "v"(voff), "s"(buffer), "s"(uniform(soff)) : "memory", "m0");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" : : "s"(uniform(dst)), "v"(voff), "s"(buffer) : "memory", "m0");
 }
 // this wavefront's LDS accesses are through, and none behind is moved ahead
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }

@@ -75,13 +75,13 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
             for (int l = 0; l < LA; ++l) {
                 unsigned v = avoff[l];
                 if (tail) v = (A_KC ? chunk * (16 / ES) : tr_k(BM, l)) < here ? v : OUTSIDE;
-                gather_lds16_at(ra, v, 0, at + l * NW * 1024);
+                gather_lds16_at(ra, v, at + l * NW * 1024);
             }
 #pragma unroll
             for (int l = 0; l < LB; ++l) {
                 unsigned v = bvoff[l];
                 if (tail) v = (B_KC ? chunk * (16 / ES) : tr_k(BN, l)) < here ? v : OUTSIDE;
-                gather_lds16_at(rb, v, 0, at + A_BYTES + l * NW * 1024);
+                gather_lds16_at(rb, v, at + A_BYTES + l * NW * 1024);
             }
         };
 #else
