@@ -112,3 +112,36 @@ def test_weight_gradient_of_several_whole_tiles_each():
         rows = slice(int(off[e]), int(off[e + 1]))
         pv, qv = p[rows].double(), q[rows].double()
         close(d[e], pv.t() @ qv, pv.abs().t() @ qv.abs(), max(1, counts[e]), "bf16")
+
+
+def test_captured_whole_tiles():
+    """A graph of a product of several whole tiles for each workgroup and of the gradient, replayed with other inputs and the program's own work in between."""
+    M, N, K, E = 4096, 8192, 1152, 4
+    v, w = variant(B.scaled_gemm_op(M, N, K, "bf16"), 256256), variant(B.grouped_wgrad_op(E, M, 2048, 4096, "bf16", "f32"), 256256)
+    if v is None:
+        return
+    v.prepare(), w.prepare()
+    g, normal = on_device(5)
+    a, sa, _ = blocks_of(normal(M, K), 1, g)
+    b, sb, _ = blocks_of(normal(N, K), 128, g)
+    c, d = torch.empty(M, N, dtype=torch.bfloat16, device="cuda"), torch.empty(E, 2048, 4096, device="cuda")
+    p, off = normal(M, 2048).bfloat16(), torch.tensor([0, 1000, 1000, 1001, 4000], dtype=torch.int32, device="cuda")
+
+    def step():
+        v.launch_static([a.data_ptr(), b.data_ptr(), sa.data_ptr(), sb.data_ptr()], c.data_ptr(), stream=devmem.current_stream())
+        w.launch_static([p.data_ptr(), c.data_ptr(), off.data_ptr()], d.data_ptr(), stream=devmem.current_stream())
+
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for _ in range(3):
+        a.copy_(blocks_of(normal(M, K), 1, g)[0])
+        got = []
+        for run in (graph.replay, step):
+            c.fill_(3), d.fill_(3)
+            run()
+            torch.cuda.synchronize()
+            got.append((c.clone(), d.clone()))
+        assert all(torch.equal(x, y) for x, y in zip(*got))
+        assert bool((got[0][1][1] == 0).all())
