@@ -141,7 +141,7 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  *                 whole: zeros for an expert without rows.
  *   Strides of the products may exceed the dense ones (rows of at most MS_MAX_ROW_BYTES); A, P and Q are shared by the experts, their stride [0] is not read.  Tensors of
  *   the products are aligned to 16 bytes (scales and offsets to 4), and several instances need copies of whole 16 bytes.
- *   Loads of 16 bytes need rows and K (P and Q: I and J) of whole 16 bytes; other sizes run a slower kernel.
+ *   Loads of 16 bytes need rows and K (P and Q: I and J) of whole 16 bytes; other sizes run a kernel that takes 7 to 18 times as long.
  */
 #define MS_EPS_UNIT 1e-12
 #define MS_MAX_EXPERTS 1024
@@ -481,7 +481,8 @@ typedef struct ms_variant_params {
     int32_t ti[4], tj[4], tc[4], tk[4]; /* the tile decisions (tc: depthwise channels) */
     int32_t tile_unit[3];   /* elements per unit of ti, tj, tk (intrinsic m, n, k; 1 for ALU) */
     int32_t block_m, block_n, block_k; /* workgroup tile in elements (depthwise: oh, ow; block_k = channels) */
-    int32_t grid[3];        /* workgroups per instance */
+    int32_t grid[3];        /* workgroups per instance (MS_BODY_RAGGED_PHASES: tiles, made by at most four workgroups for each and one for each
+                               compute unit; MS_BODY_RMS_ROWS: at most 2^20 are launched, which go on to further rows) */
     int32_t threads;        /* workgroup size */
     int32_t waves;
     int32_t acc_per_thread; /* accumulator registers per lane */

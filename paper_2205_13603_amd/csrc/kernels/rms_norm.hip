@@ -6,10 +6,10 @@
 // neighbouring lanes, whose maximum needs four cross-lane steps and no memory; the maximum is one of bit patterns without sign, which
 // order like the values and put NaN on top.
 //
-// What bounds it is memory: 16384 x 8192 in bf16 with a residual into 8 bits 171 us, 5.5 TB/s of four streams (a copy reaches 5.2 to 6.4);
-// the vector ALUs are busy 57 % of the cycles.  Results leave past the L2s, which otherwise hold lines to be written back when the kernel
-// ends (177; 16384 x 1024 28.2 -> 21.8, 8192 x 5120 bf16 without residual 38.8 -> 27).  Loads past the L2s 202; weights
-// loaded ahead of the sum 199, for the registers that they take.  One row: 4.2, the launch; 613 x 5000 7.1 back to back.
+// What bounds it is memory: 16384 x 8192 in bf16 with a residual into 8 bits 174 us, 5.4 TB/s of four streams (a copy reaches 5.2 to 6.4);
+// the vector ALUs are busy 60 % of the cycles.  Results leave past the L2s, which otherwise hold lines to be written back when the kernel
+// ends (6 us more; 16384 x 1024 28.2 -> 21.8, 8192 x 5120 bf16 without residual 38.8 -> 27).  Loads past the L2s 31 us
+// more; weights loaded ahead of the sum 28, for the registers that they take.  One row: 3.9 to 4.9, the launch; 613 x 5000 6.2 to 6.8 back to back.
 #include "common.h"
 
 struct rms_args {

@@ -807,9 +807,9 @@ int64_t ragged_rule(const ms_op *op)
 int64_t rms_rule(const ms_op *op)
 {
     // Two chunks of 8 columns for a lane while that leaves ten wavefronts to a compute unit, else the four that its registers hold (fp32:
-    // between two and three).  bf16 into 8 bits with a residual, by wavefronts to a row: 128 x 5000 8: 4.8 us, 4: 5.2, 16: 5.3; 613 x 4096
-    // 4: 5.4, 2: 6.8; 613 x 5000 4: 7.1, 8: 8.4; 2048 x 4096 2: 12.5, 4: 12.8; 16384 x 8192 4: 171, 8: 176; 16384 x 16384 8: 333, 4: 372.
-    // fp32: 2048 x 4096 4: 23.9, 2: 25.9; 16384 x 8192 8: 385, 4: 413; 613 x 5000 4: 9.7, 8: 10.9.
+    // between two and three).  bf16 into 8 bits with a residual, by wavefronts to a row: 128 x 5000 8: 4.7 us, 4: 5.6, 16: 5.8; 613 x 4096
+    // 4: 5.3, 2: 6.4; 613 x 5000 4: 6.8, 8: 7.7; 2048 x 4096 2: 11.1, 4: 12.0; 16384 x 8192 4: 176, 8: 181; 16384 x 16384 8: 342, 4: 377.
+    // fp32 into fp32: 2048 x 4096 4: 24.1, 2: 26.2; 16384 x 8192 8: 385 (5.6 TB/s), 4: 413; 613 x 5000 4: 8.3, 8: 9.3.
     auto waves = [&](int64_t columns) {
         int64_t n = 1;
         while (n < 8 && n * columns < op->K) n *= 2;
