@@ -81,7 +81,7 @@ __device__ __forceinline__ unsigned max16(unsigned x)
     o = across<0x140>(x);
     return x > o ? x : o;
 }
-// y / s in fp32 as close as the rounding to 8-bit floats can tell from a division's: the reciprocal in two parts is within 3 * 2^-48 of itself, which
+// y / s in fp32 as close as the rounding to 8-bit floats can tell from a division's: a reciprocal in two parts is within 3 * 2^-48 of the true one, which
 // leaves a quotient on its side of every tie and on the ties themselves.  (Only 518 pairs of significands have quotients so near to where the fp32
 // rounding would cross one; all of them come out as the division's.  The rounded reciprocal alone, 1.5 units off, moves one near tie in four.  16384 x 8192 in
 // bf16: 171.6 us with the reciprocal, 174.4 this way, 181 with divisions.)

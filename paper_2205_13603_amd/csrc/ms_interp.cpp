@@ -1829,6 +1829,12 @@ static inline int64_t split_index(const int32_t *f, int64_t x0, int64_t x1, int6
 
 // ---- walks of the kernels of layers: their workgroups, wavefronts and lanes
 
+static bool layer_params_fit(const ms_op *op, const ms_variant_params *p)
+{
+    if (!is_layer(op->d.kind) || (op->d.kind == MS_OP_RMS_NORM) != (p->family == MS_FAM_RMS_NORM)) return false;
+    return layer_block_fits(op, p->body_tile) && p->grid[0] > 0 && p->block_k > 0 && p->threads >= (op->d.kind == MS_OP_RMS_NORM ? 64 * p->body_tile : 64);
+}
+
 // Columns of the chunks of 8 that the lanes of a row's wavefronts take.
 template <class F> static void rms_columns(const ms_op *op, const ms_variant_params *p, F column)
 {
@@ -1935,6 +1941,7 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
     memset(counts, 0, sizeof(int32_t) * (size_t)out_elems);
     const ms_op_desc &d = op->d;
     if (is_layer_family(p->family)) {
+        if (!layer_params_fit(op, p)) return fail(MS_ERR_BAD_ARG, "ms_variant_coverage: the parameters are another operator's");
         if (p->family == MS_FAM_RMS_NORM) rms_coverage(op, p, counts);
         else ragged_coverage(op, p, counts);
         return MS_OK;
@@ -2062,6 +2069,7 @@ extern "C" int32_t ms_variant_reduction_coverage(const ms_op *op, const ms_varia
 {
     if (!op || !p) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
     if (is_layer_family(p->family)) {
+        if (!layer_params_fit(op, p)) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: the parameters are another operator's");
         if (needed) *needed = op->K;
         if (!counts) return needed ? MS_OK : fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
         if (k_elems != op->K) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: k_elems %" PRId64 " != %" PRId64, k_elems, op->K);

@@ -271,3 +271,14 @@ def test_an_eps_between_units_is_refused():
             B.rms_norm_op(4, 16, eps=eps)
     for eps, units in ((0, 0), (1e-12, 1), (1e-6, 10 ** 6), (float(np.float32(1e-5)), 10 ** 7), (1.2345e-8, 12345), (1, 10 ** 12)):
         assert B.rms_norm_op(4, 16, eps=eps).desc().dims[2] == units
+
+
+def test_coverage_refuses_the_parameters_of_another_operator():
+    norm, product = B.rms_norm_op(8, 256), B.scaled_gemm_op(40, 32, 256)
+    p, q = (B.trace_validate(op, op.space(), B.default_trace(op.space())) for op in (norm, product))
+    for op, params, n in ((norm, q, 8 * 256), (product, p, 40 * 32), (B.gemm_op(40, 32, 64), q, 40 * 32)):
+        refused(B.MS_ERR_BAD_ARG, B.variant_coverage, op, params, n)
+        refused(B.MS_ERR_BAD_ARG, B.variant_reduction_coverage, op, params)
+    for params, op, n in ((p, norm, 8 * 256), (q, product, 40 * 32)):
+        params.body_tile = 0
+        refused(B.MS_ERR_BAD_ARG, B.variant_coverage, op, params, n)
