@@ -356,7 +356,7 @@ static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *cons
         if (!inputs[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: inputs[%d] of %s is NULL", i, d.kind == MS_OP_RMS_NORM ? "the norm" : "the product");
     for (int i = 0; i < (d.kind == MS_OP_RMS_NORM ? 3 : 1); ++i)
         if (layer_has_output(op, i) && !outputs[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: outputs[%d] is NULL", i);
-    if (instances > 65535) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %d instances overflow the grid", instances);
+    if (instances > 65535 && d.kind != MS_OP_RMS_NORM) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %d instances overflow the grid", instances);
     auto aligned = [&](const void *p, int64_t to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; };
     RaggedArgs g;
     RmsArgs r;

@@ -749,3 +749,33 @@ def test_experts_of_several_instances(code):
         for e in range(E):
             rows = slice(int(off[r, e]), int(off[r, e + 1]))
             close(d[r, e], p[r, rows].double().t() @ q[r, rows].double(), p[r, rows].double().abs().t() @ q[r, rows].double().abs(), max(1, counts[r][e]), "f32")
+
+
+def test_rms_norm_in_place_beyond_the_registers():
+    """H over X and over R where most of a row is read again from H."""
+    M, N = 3, 40000
+    for kind in ("bf16", "f32"):
+        v = variant(B.rms_norm_op(M, N, kind, "f8"))
+        if v is None:
+            continue
+        g = rng(95)
+        x, w, r = normal(g, M, N).to(TYPES[kind]), (1 + normal(g, N, scale=0.1)).to(TYPES[kind]), normal(g, M, N).to(TYPES[kind])
+        want = launch_twice(v, [dev(x), dev(w), dev(r)], [((M, N), TYPES["f8"]), ((M, 313), torch.float32), ((M, N), TYPES[kind])])
+        for mine in (0, 2):
+            ts = [dev(x), dev(w), dev(r)]
+            y, s = torch.empty(M, N, dtype=TYPES["f8"], device="cuda"), torch.empty(M, 313, device="cuda")
+            v.launch([t.data_ptr() for t in ts], [y.data_ptr(), s.data_ptr(), ts[mine].data_ptr()], stream=devmem.current_stream())
+            torch.cuda.synchronize()
+            assert torch.equal(y.cpu().view(torch.uint8), want[0].view(torch.uint8)) and torch.equal(s.cpu(), want[1]) and torch.equal(ts[mine].cpu(), want[2])
+
+
+def test_rms_norm_of_more_instances_than_a_grid_has_rows():
+    M, N, R = 1, 24, 70000
+    v = variant(B.rms_norm_op(M, N, "f32", "f32", residual=False))
+    if v is None:
+        return
+    g = rng(96)
+    x, w = normal(g, R, M, N), normal(g, R, N)
+    (y, _, _) = launch_twice(v, [dev(x), dev(w), None], [((R, M, N), torch.float32), None, None], instances=R)
+    _, yv = rms_definition(x, w[:, None], None, 1e-6, "f32")
+    assert bool(((y.double() - yv).abs() <= yv.abs() * (N / 2 + 9) * 2.0 ** -24 * 1.01 + 1e-37).all())
