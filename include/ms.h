@@ -120,9 +120,10 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  * compiled kernels, and creating one for every batch costs no compilation.  stride, pad, relu and dilation are 0.
  *   RMS_NORM      dims M, N, eps in units of MS_EPS_UNIT; F32, F16 or BF16 in.  Inputs {X [M][N], W [N], R [M][N] or NULL}, outputs
  *                 {Y [M][N], S, H}.  has_bias 1: a residual R is added, H [M][N] = X + R rounded once to in_dtype, and the norm is that of
- *                 the rounded H, so that it can be computed again from what is kept; H is dense: it may be R itself, and X
- *                 itself where a_strides[1] is N (M > 1; other launches are refused).  has_bias 0: R and H are not read, H = X.  y = h / sqrt(sum(h^2) / N + eps) * w in fp32.  out_dtype = in_dtype: Y = y rounded once, S is not
- *                 read.  out_dtype F8E4M3: with S[i][b] = max(max_{128 columns of block b} |y| / 448, 2^-126) (fp32, [M][ceil(N / 128)]) Y is y / S, the quotient
+ *                 the rounded H, so that it can be computed again from what is kept.  H is dense: it may be R
+ *                 itself, and X itself where that is dense too (one row, or a_strides[1] = N; a launch with another X is refused).  has_bias 0:
+ *                 R and H are not read, H = X.  y = h / sqrt(sum(h^2) / N + eps) * w in fp32.  out_dtype = in_dtype: Y = y rounded once, S is
+ *                 not read.  out_dtype F8E4M3: with S[i][b] = max(max_{128 columns of block b} |y| / 448, 2^-126) (fp32, [M][ceil(N / 128)]) Y is y / S, the quotient
  *                 in fp32, rounded (to the nearest 8-bit float, ties to even); a NaN in a block makes S and the block NaN.  a_strides[1] = elements between rows of X (0 = N);
  *                 b_strides 0.  Tensors need only be aligned to their elements.
  *   SCALED_GEMM   dims M, N, K; in F8E4M3, out F16, BF16 or F32.  Inputs {A [M][K], B [N][K], SA fp32 [M][ceil(K / 128)],
