@@ -85,7 +85,8 @@ def draw(rng):
                 backward = rng.random() < 0.4
                 scores = rng.choice(["softmax", "sigmoid"])
                 case |= {"backward": backward, "type": rng.choice(["f32", "bf16", "f16"]), "scores": scores, "bias": not backward and rng.random() < 0.5, "groups": groups,
-                         "kept": rng.randrange(1, groups + 1), "best": rng.choice([1, 2]) if groups > 1 else 1, "renormalise": rng.random() < 0.6, "scale": rng.choice([1.0, 2.5])}
+                         "kept": rng.randrange(1, groups + 1), "best": rng.choice([1, 2]) if groups > 1 else 1, "renormalise": rng.random() < 0.6 and not (backward and chosen == 1),  # constant weights have no gradient
+                         "scale": rng.choice([1.0, 2.5])}
             elif op == "rows":
                 way, kind = rng.choice(["out", "back", "grad"]), rng.choice(["bf16", "bf16", "f16", "f32"])
                 case |= {"way": way, "cols": _spread(rng, 64, 8192, rng.choice([1, 8, 128])), "type": kind, "out": rng.choice(["i8", kind]) if way == "out" else kind,
@@ -248,7 +249,7 @@ def _route_grad(s):
     if case["renormalise"]:
         p = score.gather(1, ids) * real
         total = torch.where(real.any(-1, keepdim=True), p.sum(-1, keepdim=True), 1.0)
-        g = (g - (g * p).sum(-1, keepdim=True) / total) / total * real
+        g = (g - (g * (p / total)).sum(-1, keepdim=True)) / total * real
     d = torch.zeros_like(x).scatter_add_(1, ids, g)
     d = score * (d - (d * score).sum(-1, keepdim=True)) if case["scores"] == "softmax" else d * score * (1 - score)
     return d.to(s["logits"].dtype)
