@@ -79,7 +79,7 @@ typedef enum ms_op_kind {
     MS_OP_CONV3D_NDHWC = 9,  /* Y = act(bias + conv(X, W)), X [N][D][H][W][Cin], W [K][K][K][Cin][Cout]  (C3D) */
     /* layers of language models: one kernel for all sizes, see below */
     MS_OP_RMS_NORM = 10,     /* H = X + R, Y = quantise(H / sqrt(mean(H^2) + eps) * W) */
-    MS_OP_SCALED_GEMM = 11,  /* C[i][j] = sum_b SA[i][b] SB[j/128][b] sum_{k in block b of 128} A[i][k] B[j][k] */
+    MS_OP_SCALED_GEMM = 11,  /* C[i][j] = sum_b SA[i][b] SB[j/128][b] sum_{k in block b of 128} A[i][k] B[j][k], or SA[i] SB[j] sum_k A[i][k] B[j][k] */
     MS_OP_GROUPED_GEMM = 12, /* C[t][j] = sum_k A[t][k] B[e(t)][k][j], rows t sorted by expert e */
     MS_OP_GROUPED_WGRAD = 13 /* D[e][i][j] = sum_{t of expert e} P[t][i] Q[t][j]: the gradient of B above */
 } ms_op_kind;
@@ -133,8 +133,10 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  *                 of the largest one's power of two, and adds the sums of the eights in fp32.  A block is off by less than 7 * 2^-13 of its eights'
  *                 largest magnitudes added up; with normally distributed operands 2^-16 of the sum of all magnitudes, 1.3e-5 of the results' root
  *                 mean square.  F32 results are no more exact than that; F16 and BF16 lose more by their own rounding unless sums cancel or few products dominate.
- *   GROUPED_GEMM  dims E, T, N, K (E <= MS_MAX_EXPERTS); F16 or BF16 in, the same or F32 out, or F8E4M3 as above.  Inputs {A [T][K], B [E][N][K],
- *                 offsets int32 [E + 1] (device memory), SA [T][ceil(K / 128)], SB [E][ceil(N / 128)][ceil(K / 128)]} (the scales for F8E4M3 only).  Expert e has
+ *                 I8 in (a scale for each token and each channel): SA fp32 [M], SB fp32 [N]; the sum is exact (K <= MS_MAX_I8_DEPTH), rounded to
+ *                 fp32, times SA[i], times SB[j], each rounded to fp32, and rounded to the output type.
+ *   GROUPED_GEMM  dims E, T, N, K (E <= MS_MAX_EXPERTS); F16 or BF16 in, the same or F32 out, or F8E4M3 and I8 as above.  Inputs {A [T][K], B [E][N][K],
+ *                 offsets int32 [E + 1] (device memory), SA [T][ceil(K / 128)], SB [E][ceil(N / 128)][ceil(K / 128)]} (the scales for F8E4M3; I8: SA [T], SB [E][N]).  Expert e has
  *                 the rows from offsets[e] up to offsets[e + 1] (none if that is not larger) of A and C; rows of no expert are left as they were in C.
  *                 offsets do not decrease; values outside [0, T] count as the nearer end.  b_strides {N * K, 1, K} (the default) or, 2-byte inputs,
  *                 {K * N, N, 1}: B stored [E][K][N], as the gradient of A needs it.
@@ -146,6 +148,7 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  */
 #define MS_EPS_UNIT 1e-12
 #define MS_MAX_EXPERTS 1024
+#define MS_MAX_I8_DEPTH 131071 /* products of up to 2^14 in sums of 32 bits */
 #define MS_MAX_ROW_BYTES (4 << 20)
 typedef struct ms_op_desc {
     int32_t kind;

@@ -28,7 +28,7 @@ STATIC_WORKSPACE_BYTES = 32 << 20
 FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE, FAM_RMS_NORM, FAM_RAGGED = range(6)
 (BODY_NEST, BODY_ROW_VECTORS, BODY_STRIPS, BODY_IMAGE_ROWS, BODY_PHASES, BODY_DOUBLE_STEPS, BODY_CONV_STEPS, BODY_CONV_PATCH, BODY_CONV_PLANES,
  BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS, BODY_RAGGED_PHASES) = range(14)
-EPS_UNIT, MAX_EXPERTS, SCALE_BLOCK = 1e-12, 1024, 128
+EPS_UNIT, MAX_EXPERTS, MAX_I8_DEPTH, SCALE_BLOCK = 1e-12, 1024, 131071, 128
 LAYERS = (OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD)
 MAX_SLOTS, MAX_FACTORS, MAX_CANDS, MAX_LOOPS = 16, 4, 12, 8
 
@@ -369,17 +369,18 @@ def rms_norm_op(M, N, in_dtype="bf16", out_dtype=None, residual=True, eps=1e-6, 
     return Op(OP_RMS_NORM, in_dtype, out_dtype or in_dtype, [M, N, units], has_bias=residual, **kw)
 
 
-def scaled_gemm_op(M, N, K, out_dtype="bf16", **kw):
-    """C [M, N] of 8-bit floats A [M, K] and B [N, K] with scales SA [M, ceil(K / 128)], SB [ceil(N / 128), ceil(K / 128)]; inputs (A, B, SA, SB)."""
-    return Op(OP_SCALED_GEMM, "f8", out_dtype, [M, N, K], **kw)
+def scaled_gemm_op(M, N, K, out_dtype="bf16", in_dtype="f8", **kw):
+    """C [M, N] of 8-bit floats A [M, K] and B [N, K] with scales SA [M, ceil(K / 128)], SB [ceil(N / 128), ceil(K / 128)], or of 8-bit integers
+    ("i8") with a scale for each row, SA [M], and each column, SB [N]; inputs (A, B, SA, SB)."""
+    return Op(OP_SCALED_GEMM, in_dtype, out_dtype, [M, N, K], **kw)
 
 
 def grouped_gemm_op(E, T, N, K, rows_of_k=True, in_dtype="bf16", out_dtype=None, **kw):
     """C [T, N]: rows of A [T, K], sorted by expert, times their expert's matrix of B [E, N, K] (rows_of_k) or [E, K, N]; inputs
-    (A, B, offsets int32 [E + 1]), for "f8" also (SA, SB)."""
+    (A, B, offsets int32 [E + 1]), for "f8" and "i8" also (SA, SB), those of "i8" [T] and [E, N]."""
     if not rows_of_k and "b_strides" not in kw:
         kw["b_strides"] = [K * N, N, 1]
-    return Op(OP_GROUPED_GEMM, in_dtype, out_dtype or ("bf16" if in_dtype == "f8" else in_dtype), [E, T, N, K], **kw)
+    return Op(OP_GROUPED_GEMM, in_dtype, out_dtype or ("bf16" if in_dtype in ("f8", "i8") else in_dtype), [E, T, N, K], **kw)
 
 
 def grouped_wgrad_op(E, T, I, J, in_dtype="bf16", out_dtype=None, **kw):

@@ -1,6 +1,7 @@
 // Products over rows that lie sorted by expert (or of one matrix), and the gradient of the experts' matrices, on the matrix cores.
 //
 //   C[t][j]    = sum_k A[t][k] B[e(t)][k][j]        8-bit floats: sum over blocks of 128 k of SA[t][b] SB[e][j/128][b] (block's sum)
+//                                                   8-bit integers: the sum, exact in 32 bits, times SA[t] SB[e][j]
 //   D[e][i][j] = sum over the rows t of e of P[t][i] Q[t][j]                                                     (WGRAD)
 //
 // A workgroup makes one tile of rows of one expert (ragged_tile.h).  Two or three lie on a compute unit and overlap each other's loads, products

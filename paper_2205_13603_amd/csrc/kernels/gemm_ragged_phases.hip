@@ -239,12 +239,12 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     lt = none;
 
     // ---- fragments
-    f4_t acc[TM][TN];
+    sum4_t acc[TM][TN];
     frag_t fa[KQ][TM / 2], fb[KQ][TN];
     float fs[TM / 2];
     auto frag_kc = [&](const char *p, int q) {
         frag_t f;
-        if (ES == 2) {
+        if (KQ == 2) {
             f.v[0] = *reinterpret_cast<const u4_t *>(p + ((q * 4 + lgrp) ^ lrow % 8) * 16);
         } else {
 #pragma unroll
@@ -324,12 +324,20 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+            for (int j = 0; j < TN; ++j) acc[i][j] = sum4_t{0, 0, 0, 0};
     };
     auto store = [&](const tile_t &t) {
         const int lane = opaque(tid % 64), lrow = lane % 16, lgrp = lane / 16;
         char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
         const int cols = g.cols - t.col < BN ? g.cols - t.col : BN;
+        const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + t.row;
+        const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)t.expert * g.cols + t.col;
+        f4_t sj[TN];
+        float si[TM];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sj[j] = col_scales(of_cols, wj * 64 + j * 16 + lgrp * 4, cols);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) si[i] = row_scale(of_rows, wi * 128 + i * 16 + lrow, t.rows);
         if constexpr (OS == 4) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
@@ -338,7 +346,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const int col = wj * 64 + j * 16 + lgrp * 4;
-                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, acc[i][j], cols - col);
+                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
                     }
                 }
             }
@@ -354,8 +362,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
                         for (int j = 0; j < TN; ++j) {
                             quad_t o;
+                            const f4_t x = results(acc[i][j], si[i], sj[j]);
 #pragma unroll
-                            for (int v = 0; v < 4; ++v) o.v[v] = from_acc(acc[i][j][v]);
+                            for (int v = 0; v < 4; ++v) o.v[v] = round_out(x[v]);
                             *reinterpret_cast<quad_t *>(mine + lrow % 8 * 128 + ((j * 2 + lgrp / 2) ^ lrow % 8) * 16 + lgrp % 2 * 8) = o;
                         }
                     }

@@ -1,6 +1,7 @@
 // Products of few rows (of each expert) with matrices whose rows run along k: a decoding step.
 //
 //   C[t][j] = sum_k A[t][k] B[e(t)][j][k]           8-bit floats: sum over blocks of 128 k of SA[t][b] SB[e][j/128][b] (block's sum)
+//                                                   8-bit integers: the sum, exact in 32 bits, times SA[t] SB[e][j]
 //
 // What bounds it is reading B once.  The wavefronts of a workgroup split the reduction of its BM x BN tile, blocks of 128 bytes in
 // turn, and add their sums up in LDS at the end, in the order of their numbers.  Each has a ring of LDS stages of its own, which
@@ -75,11 +76,11 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         gather_lds4(sb, lane == 0 ? (unsigned)k * 4 : OUTSIDE, at + (BM + BN) * 128 + 256);
 #endif
     };
-    f4_t acc[MT][NC];
+    sum4_t acc[MT][NC];
 #pragma unroll
     for (int i = 0; i < MT; ++i)
 #pragma unroll
-        for (int j = 0; j < NC; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+        for (int j = 0; j < NC; ++j) acc[i][j] = sum4_t{0, 0, 0, 0};
 
 #pragma unroll
     for (int s = 0; s < STAGES; ++s)
@@ -95,7 +96,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         frag_t fa[KQ][MT], fb[KQ][NC];
         auto frag = [&](const char *r, int q) {
             frag_t f;
-            if (ES == 2) {
+            if (KQ == 2) {
                 f.v[0] = *reinterpret_cast<const u4_t *>(r + ((q * 4 + lgrp) ^ lrow % 8) * 16);
             } else {
 #pragma unroll
@@ -140,21 +141,26 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
     for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int j = 0; j < NC; ++j) *reinterpret_cast<f4_t *>(lds + ((wave * MT + m) * NC + j) * 1024 + lane * 16) = acc[m][j];
+        for (int j = 0; j < NC; ++j) *reinterpret_cast<sum4_t *>(lds + ((wave * MT + m) * NC + j) * 1024 + lane * 16) = acc[m][j];
     barrier();
     char *c = g.c + inst * g.c_inst;
+    const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + row;
+    const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)expert * g.cols + col;
 #pragma unroll
     for (int i = 0; i < (MT * NC + NW - 1) / NW; ++i) {
         const int tile = i * NW + wave;
         if (tile >= MT * NC) break;
-        f4_t sum = f4_t{0, 0, 0, 0};
+        sum4_t sum = sum4_t{0, 0, 0, 0};
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            const f4_t x = *reinterpret_cast<const f4_t *>(lds + (w * MT * NC + tile) * 1024 + lane * 16);
+            const sum4_t x = *reinterpret_cast<const sum4_t *>(lds + (w * MT * NC + tile) * 1024 + lane * 16);
 #pragma unroll
             for (int v = 0; v < 4; ++v) sum[v] += x[v];
         }
         const int r = tile / NC * 16 + lrow, j = tile % NC * 16 + lgrp * 4;
-        if (r < rows && j < cols) store4<false>(c + ((long)(row + r) * g.cols + col + j) * (long)sizeof(out_t), sum, cols - j);
+        if (r < rows && j < cols) {
+            const f4_t x = results(sum, row_scale(of_rows, r, rows), col_scales(of_cols, j, cols));
+            store4<false>(c + ((long)(row + r) * g.cols + col + j) * (long)sizeof(out_t), x, cols - j);
+        }
     }
 }

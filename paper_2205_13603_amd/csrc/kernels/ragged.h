@@ -17,6 +17,12 @@ typedef float f4_t __attribute__((ext_vector_type(4)));
 typedef _Float16 h8_t __attribute__((ext_vector_type(8)));
 typedef __bf16 b8_t __attribute__((ext_vector_type(8)));
 typedef int i8v_t __attribute__((ext_vector_type(8)));
+typedef int i4_t __attribute__((ext_vector_type(4)));
+#if IN_DT == DT_I8
+typedef i4_t sum4_t; // 8-bit integers are summed exactly
+#else
+typedef f4_t sum4_t;
+#endif
 
 // One matrix-core step.  The operands are swapped, so that a lane holds four consecutive columns of one row: rows lane % 16, columns
 // 4 * (lane / 16) and on.
@@ -29,17 +35,63 @@ __device__ __forceinline__ f4_t mfma(const frag_t &b, const frag_t &a, f4_t c)
     return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(__builtin_bit_cast(i8v_t, b), __builtin_bit_cast(i8v_t, a), c, 0, 0, 0, 0, 0, 0);
 }
 #else
-struct frag_t { u4_t v[1]; }; // 8 k values
-__device__ __forceinline__ f4_t mfma(const frag_t &b, const frag_t &a, f4_t c)
+struct frag_t { u4_t v[1]; }; // 8 k values, of 8-bit integers 16
+__device__ __forceinline__ sum4_t mfma(const frag_t &b, const frag_t &a, sum4_t c)
 {
-#if IN_DT == DT_F16
+#if IN_DT == DT_I8
+    return __builtin_amdgcn_mfma_i32_16x16x64_i8(__builtin_bit_cast(i4_t, b.v[0]), __builtin_bit_cast(i4_t, a.v[0]), c, 0, 0, 0);
+#elif IN_DT == DT_F16
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8_t, b.v[0]), __builtin_bit_cast(h8_t, a.v[0]), c, 0, 0, 0);
 #else
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8_t, b.v[0]), __builtin_bit_cast(b8_t, a.v[0]), c, 0, 0, 0);
 #endif
 }
 #endif
-constexpr int ES = sizeof(in_t), KQ = ES == 2 ? 2 : 1; // matrix-core steps of a k step of 128 bytes
+constexpr int ES = sizeof(in_t), KQ = 8 / (sizeof(frag_t) / 4); // matrix-core steps of a k step of 128 bytes
+static_assert(KQ == (IN_DT == DT_F8E4M3 ? 1 : 2), "16 bytes of a row for each lane, or 32");
+
+// The one rounding to the output type.
+__device__ __forceinline__ out_t round_out(float x)
+{
+#if OUT_DT == DT_BF16
+    return float_to_bf16(x);
+#else
+    return (out_t)x;
+#endif
+}
+
+// Sums as results.  8-bit integers: times the scale of their row, then those of their columns (in this order no product of two small scales
+// is formed); the sum is rounded to fp32 first, each product once: 3 * 2^-24 in all.
+__device__ __forceinline__ f4_t results(const sum4_t &x, float of_row, const f4_t &of_cols)
+{
+#if IN_DT == DT_I8
+    f4_t y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = (float)x[i] * of_row * of_cols[i];
+    return y;
+#else
+    return x;
+#endif
+}
+// Scales of 8-bit integers: of row r of `rows` from `sa`, of four columns from `sb` (1 for what is not there).
+__device__ __forceinline__ float row_scale(const float *sa, int r, int rows)
+{
+#if IN_DT == DT_I8
+    return r < rows ? sa[r] : 1.f;
+#else
+    return 1.f;
+#endif
+}
+__device__ __forceinline__ f4_t col_scales(const float *sb, int col, int cols)
+{
+    f4_t s = {1.f, 1.f, 1.f, 1.f};
+#if IN_DT == DT_I8
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (col + i < cols) s[i] = sb[col + i];
+#endif
+    return s;
+}
 
 // A barrier of the workgroup that the compiler moves no memory access across; this wavefront's LDS accesses are through before it.
 __device__ __forceinline__ void barrier()
@@ -253,7 +305,7 @@ template <bool STREAM> __device__ __forceinline__ void store4(char *dst, f4_t x,
     struct __attribute__((packed, aligned(sizeof(out_t)))) quad { out_t v[4]; };
     quad q;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q.v[i] = from_acc(x[i]);
+    for (int i = 0; i < 4; ++i) q.v[i] = round_out(x[i]);
     if (n >= 4) {
         if (STREAM) stream_out(dst, q);
         else *reinterpret_cast<quad *>(dst) = q;

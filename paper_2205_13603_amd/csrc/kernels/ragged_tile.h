@@ -136,18 +136,18 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
         };
 #endif
 
-        f4_t acc[TM][TN];
+        sum4_t acc[TM][TN];
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-            for (int j = 0; j < TN; ++j) acc[i][j] = f4_t{0, 0, 0, 0};
+            for (int j = 0; j < TN; ++j) acc[i][j] = sum4_t{0, 0, 0, 0};
 
         // ---- fragments
         // of 16 rows from `row0` of a k-contiguous operand at `p`, matrix-core step q
         auto frag_kc = [&](const char *p, int row0, int q) {
             frag_t f;
             const char *r = p + row0 * 128 + lrow * 128;
-            if (ES == 2) {
+            if (KQ == 2) {
                 f.v[0] = *reinterpret_cast<const u4_t *>(r + ((q * 4 + lgrp) ^ lrow % 8) * 16);
             } else {
 #pragma unroll
@@ -271,8 +271,8 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
             }
             if (!group) barrier();
             // each group's half of the sums: its own and the other's
-            auto of = [&](f4_t one, f4_t zero) { // values, not places: chosen by address the sums would lie in memory
-                f4_t x;
+            auto of = [&](sum4_t one, sum4_t zero) { // values, not places: chosen by address the sums would lie in memory
+                sum4_t x;
 #pragma unroll
                 for (int v = 0; v < 4; ++v) x[v] = group ? one[v] : zero[v];
                 return x;
@@ -283,13 +283,13 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
 #pragma unroll
             for (int i = 0; i < TM / 2; ++i)
 #pragma unroll
-                for (int j = 0; j < TN; ++j) *reinterpret_cast<f4_t *>(other + (i * TN + j) * 1024) = of(acc[i][j], acc[TM / 2 + i][j]);
+                for (int j = 0; j < TN; ++j) *reinterpret_cast<sum4_t *>(other + (i * TN + j) * 1024) = of(acc[i][j], acc[TM / 2 + i][j]);
             barrier();
 #pragma unroll
             for (int i = 0; i < TM / 2; ++i)
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
-                    const f4_t x = *reinterpret_cast<const f4_t *>(here + (i * TN + j) * 1024), y = of(acc[TM / 2 + i][j], acc[i][j]);
+                    const sum4_t x = *reinterpret_cast<const sum4_t *>(here + (i * TN + j) * 1024), y = of(acc[TM / 2 + i][j], acc[i][j]);
 #pragma unroll
                     for (int v = 0; v < 4; ++v) acc[i][j][v] = y[v] + x[v];
                 }
@@ -300,6 +300,14 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
         constexpr int OS = sizeof(out_t), HALF = TM / GROUPS; // row tiles that this wavefront stores
         const int row0 = (wi * TM + group * HALF) * 16;
         char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
+        const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + t.row;
+        const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)t.expert * g.cols + t.col;
+        f4_t sj[TN];
+        float si[HALF];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sj[j] = col_scales(of_cols, (wj * TN + j) * 16 + lgrp * 4, cols);
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) si[i] = row_scale(of_rows, row0 + i * 16 + lrow, t.rows);
         if constexpr (OS == 4) {
 #pragma unroll
             for (int i = 0; i < HALF; ++i) {
@@ -308,7 +316,7 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
 #pragma unroll
                     for (int j = 0; j < TN; ++j) {
                         const int col = (wj * TN + j) * 16 + lgrp * 4;
-                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, acc[i][j], cols - col);
+                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
                     }
                 }
             }
@@ -324,8 +332,9 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
 #pragma unroll
                 for (int j = 0; j < TN; ++j) {
                     struct { out_t v[4]; } o;
+                    const f4_t x = results(acc[i][j], si[i], sj[j]);
 #pragma unroll
-                    for (int v = 0; v < 4; ++v) o.v[v] = from_acc(acc[i][j][v]);
+                    for (int v = 0; v < 4; ++v) o.v[v] = round_out(x[v]);
                     *reinterpret_cast<decltype(o) *>(mine + (lrow * CH + ((j * 2 + lgrp / 2) ^ (lrow % CH))) * 16 + lgrp % 2 * 8) = o;
                 }
                 lds_done();

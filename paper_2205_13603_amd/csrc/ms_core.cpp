@@ -200,10 +200,10 @@ static int32_t create_layer(const ms_op_desc &d, ms_op *op)
         return fail(MS_ERR_BAD_ARG, "ms_op_create: stride/pad/bias/relu/dilation do not apply to %s", op_kind_name(d.kind));
     if (d.has_bias != 0 && d.has_bias != 1) return fail(MS_ERR_BAD_ARG, "ms_op_create: has_bias = %d", d.has_bias);
     if (!dtype_size(d.in_dtype) || !dtype_size(d.out_dtype)) return fail(MS_ERR_BAD_ARG, "ms_op_create: bad dtype %d or %d", d.in_dtype, d.out_dtype);
-    const bool half = d.in_dtype == MS_F16 || d.in_dtype == MS_BF16, f8 = d.in_dtype == MS_F8E4M3;
+    const bool half = d.in_dtype == MS_F16 || d.in_dtype == MS_BF16, f8 = d.in_dtype == MS_F8E4M3, i8 = d.in_dtype == MS_I8;
     bool ok;
     if (d.kind == MS_OP_RMS_NORM) ok = (half || d.in_dtype == MS_F32) && (d.out_dtype == d.in_dtype || d.out_dtype == MS_F8E4M3);
-    else if (f8) ok = d.kind != MS_OP_GROUPED_WGRAD && (d.out_dtype == MS_F16 || d.out_dtype == MS_BF16 || d.out_dtype == MS_F32);
+    else if (f8 || i8) ok = d.kind != MS_OP_GROUPED_WGRAD && (d.out_dtype == MS_F16 || d.out_dtype == MS_BF16 || d.out_dtype == MS_F32);
     else ok = d.kind != MS_OP_SCALED_GEMM && half && (d.out_dtype == d.in_dtype || d.out_dtype == MS_F32);
     if (!ok)
         return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s with in %s -> out %s is not supported", op_kind_name(d.kind), dtype_name(d.in_dtype), dtype_name(d.out_dtype));
@@ -245,7 +245,8 @@ static int32_t create_layer(const ms_op_desc &d, ms_op *op)
         if (b_zero) b[0] = op->N * op->K, b[1] = 1, b[2] = op->K;
         const bool by_k = b[1] == 1 && b[2] >= op->K, by_j = b[2] == 1 && b[1] >= op->N;
         if (a[2] != 1 || a[1] < op->K) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s takes rows of A contiguous along k that do not overlap", op_kind_name(d.kind));
-        if (!by_k && (!by_j || f8)) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s takes B contiguous along k%s, its rows not overlapping", op_kind_name(d.kind), f8 ? "" : " or j");
+        if (!by_k && (!by_j || f8 || i8)) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: %s takes B contiguous along k%s, its rows not overlapping", op_kind_name(d.kind), f8 || i8 ? "" : " or j");
+        if (i8 && op->K > MS_MAX_I8_DEPTH) return fail(MS_ERR_UNSUPPORTED, "ms_op_create: sums of %" PRId64 " products of 8-bit integers, at most %d", op->K, MS_MAX_I8_DEPTH);
         if (op->nb > 1 && b[0] < (by_k ? (op->N - 1) * b[2] + op->K : (op->K - 1) * b[1] + op->N)) return fail(MS_ERR_BAD_ARG, "ms_op_create: matrices of B overlap");
         if (a[1] > most_row || (by_k ? b[2] : b[1]) > most_row || (by_k ? op->K : op->N) > most_row)
             return fail(MS_ERR_UNSUPPORTED, "ms_op_create: rows of more than %d bytes", MS_MAX_ROW_BYTES);
@@ -540,8 +541,8 @@ extern "C" int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx, int64_t *byt
         else if (idx == 0) e = (op->M - 1) * d.a_strides[1] + op->K;
         else if (idx == 1) e = (op->nb - 1) * d.b_strides[0] + (op->K - 1) * d.b_strides[1] + (op->N - 1) * d.b_strides[2] + 1;
         else if (idx == 2 && at == 3) sz = 4, e = op->nb + 1;
-        else if (idx == at && d.in_dtype == MS_F8E4M3) sz = 4, e = op->M * scale_blocks(op->K);
-        else if (idx == at + 1 && d.in_dtype == MS_F8E4M3) sz = 4, e = op->nb * scale_blocks(op->N) * scale_blocks(op->K);
+        else if (idx == at && has_scales(d)) sz = 4, e = op->M * (d.in_dtype == MS_I8 ? 1 : scale_blocks(op->K));
+        else if (idx == at + 1 && has_scales(d)) sz = 4, e = op->nb * (d.in_dtype == MS_I8 ? op->N : scale_blocks(op->N) * scale_blocks(op->K));
         break;
     }
     case MS_OP_GROUPED_WGRAD:
@@ -609,6 +610,7 @@ extern "C" int32_t ms_op_work(const ms_op *op, double *flop, double *bytes)
         f = 2.0 * op->M * op->N * op->K;
         b = ((double)op->M * op->K + (double)op->nb * op->N * op->K) * op->in_size + (double)op->M * op->N * op->out_size;
         if (d.in_dtype == MS_F8E4M3) b += 4.0 * scale_blocks(op->K) * ((double)op->M + (double)op->nb * scale_blocks(op->N));
+        if (d.in_dtype == MS_I8) b += 4.0 * ((double)op->M + (double)op->nb * op->N);
         if (d.kind == MS_OP_GROUPED_GEMM) b += 4.0 * (op->nb + 1);
         break;
     case MS_OP_GROUPED_WGRAD:

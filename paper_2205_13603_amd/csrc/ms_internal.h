@@ -33,6 +33,8 @@ inline bool follows_decisions(const ms_variant_params *p)
 // Layers of language models: sizes are arguments of their kernels
 inline bool is_layer(int32_t kind) { return kind >= MS_OP_RMS_NORM && kind <= MS_OP_GROUPED_WGRAD; }
 inline bool is_layer_family(int32_t family) { return family == MS_FAM_RMS_NORM || family == MS_FAM_RAGGED; }
+// products whose operands come with scales: for blocks of 128 k values, of 8-bit integers for rows and columns
+inline bool has_scales(const ms_op_desc &d) { return d.in_dtype == MS_F8E4M3 || d.in_dtype == MS_I8; }
 inline int64_t scale_blocks(int64_t n) { return (n + 127) / 128; }
 // What a launch hands to the kernels of layers; the same structs stand in ragged.h and rms_norm.hip.  Rows and distances in bytes.
 struct RaggedArgs {

@@ -730,7 +730,7 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
     t.bn = (int)(code % 1000);
     t.few = t.bn <= 32;
     t.groups = 1;
-    const bool scaled = op->in_size == 1, table = op->d.kind == MS_OP_GROUPED_GEMM;
+    const bool scaled = op->d.in_dtype == MS_F8E4M3, table = op->d.kind == MS_OP_GROUPED_GEMM;
     const bool alone = ragged_expected(op, t) <= 256; // each workgroup has a compute unit to itself
     if (t.few) {
         // Where each workgroup has a compute unit to itself, eight wavefronts share its reduction (10 x 256 x 13312 in 8 bits: 9.0 -> 6.6 us,
@@ -782,7 +782,7 @@ int64_t ragged_rule(const ms_op *op)
     const double bytes = wgrad ? 0 : (double)matrices * (double)op->N * (double)op->K * op->in_size;
     int64_t best = 0;
     double least = 0;
-    for (const auto &c : costs[op->in_size == 1 ? 0 : 1]) {
+    for (const auto &c : costs[op->d.in_dtype == MS_F8E4M3 ? 0 : 1]) { // 8-bit integers: as many matrix-core cycles to a step as 16-bit floats
         if (!layer_block_fits(op, c.code)) continue;
         const RaggedTile t = ragged_tile(op, c.code);
         const double more = wgrad && many ? 1 : 0; // a gradient's tiles are as long as their experts: one more
@@ -851,7 +851,7 @@ int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *tr
         p->waves = t.wi * t.wj * t.groups;
         p->threads = p->waves * 64;
         p->tile_unit[0] = p->tile_unit[1] = 16;
-        p->tile_unit[2] = op->in_size == 1 ? 128 : 32;
+        p->tile_unit[2] = op->d.in_dtype == MS_F8E4M3 ? 128 : op->d.in_dtype == MS_I8 ? 64 : 32;
         p->mfma = MS_MFMA_CODE(16, 16, p->tile_unit[2]);
         p->acc_per_thread = t.few ? t.bm * t.bn / 64 : t.bm * t.bn / (t.wi * t.wj * 64);
         p->vec = p->vec_b = aligned ? 16 / op->in_size : 1;
@@ -1519,7 +1519,7 @@ bool ms::layer_block_fits(const ms_op *op, int64_t code)
     const bool few = code % 1000 <= 32;
     if (!ragged_aligned(op)) return code == 64128;
     if (few) return ragged_by_k(op) && (code == 16016 || code == 16032 || code == 32032 || code == 64032);
-    if (code == 256256) return op->in_size == 2 || op->K > 128; // a single block's scales would be a run of one step (ragged_schedule.h)
+    if (code == 256256) return op->d.in_dtype != MS_F8E4M3 || op->K > 128; // a single block's scales would be a run of one step (ragged_schedule.h)
     return code == 64128 || code == 128128;
 }
 

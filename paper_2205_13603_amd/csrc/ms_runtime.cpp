@@ -334,7 +334,7 @@ static int32_t load_layer(ms_variant *v, int dev, const LoadedKernel **loaded)
 // Inputs and outputs of a layer in the order of ms_op_desc: how many, and which may be NULL.
 static int layer_inputs(const ms_op &op)
 {
-    const bool scaled = op.d.in_dtype == MS_F8E4M3;
+    const bool scaled = has_scales(op.d);
     switch (op.d.kind) {
     case MS_OP_RMS_NORM: return 2 + op.d.has_bias;
     case MS_OP_SCALED_GEMM: return 4;
@@ -376,7 +376,7 @@ static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *cons
         args[0] = &r;
     } else {
         const int at = d.kind == MS_OP_SCALED_GEMM ? 2 : 3; // of the scales
-        const bool scaled = d.in_dtype == MS_F8E4M3, grouped = d.kind != MS_OP_SCALED_GEMM;
+        const bool scaled = has_scales(d), grouped = d.kind != MS_OP_SCALED_GEMM;
         const void *offsets = grouped ? inputs[2] : nullptr, *sa = scaled ? inputs[at] : nullptr, *sb = scaled ? inputs[at + 1] : nullptr;
         if (!aligned(inputs[0], 16) || !aligned(inputs[1], 16) || !aligned(outputs[0], 16))
             return fail(MS_ERR_BAD_ARG, "ms_variant_launch: the product's tensors must be 16-byte aligned");
