@@ -81,7 +81,14 @@ typedef enum ms_op_kind {
     MS_OP_RMS_NORM = 10,     /* H = X + R, Y = quantise(H / sqrt(mean(H^2) + eps) * W) */
     MS_OP_SCALED_GEMM = 11,  /* C[i][j] = sum_b SA[i][b] SB[j/128][b] sum_{k in block b of 128} A[i][k] B[j][k], or SA[i] SB[j] sum_k A[i][k] B[j][k] */
     MS_OP_GROUPED_GEMM = 12, /* C[t][j] = sum_k A[t][k] B[e(t)][k][j], rows t sorted by expert e */
-    MS_OP_GROUPED_WGRAD = 13 /* D[e][i][j] = sum_{t of expert e} P[t][i] Q[t][j]: the gradient of B above */
+    MS_OP_GROUPED_WGRAD = 13,/* D[e][i][j] = sum_{t of expert e} P[t][i] Q[t][j]: the gradient of B above */
+    /* routing to experts, around the products above: likewise */
+    MS_OP_ROUTE = 14,        /* which experts a token goes to, and with which weights */
+    MS_OP_ROUTE_GRAD = 15,   /* the gradient of its logits */
+    MS_OP_EXPERT_ORDER = 16, /* the choices sorted by expert: offsets, and the row of each */
+    MS_OP_SPREAD_ROWS = 17,  /* A[place[t][j]] = X[t], quantised where A has 8 bits */
+    MS_OP_JOIN_ROWS = 18,    /* Y[t] = R[t] + sum_j W[t][j] C[place[t][j]] */
+    MS_OP_JOIN_GRAD = 19     /* the gradients of C and W above */
 } ms_op_kind;
 
 typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 = 4,
@@ -145,8 +152,42 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  *   Strides of the products may exceed the dense ones (rows of at most MS_MAX_ROW_BYTES); A, P and Q are shared by the experts, their stride [0] is not read.  Tensors of
  *   the products are aligned to 16 bytes (scales and offsets to 4), and several instances need copies of whole 16 bytes.
  *   Loads of 16 bytes need rows and K (P and Q: I and J) of whole 16 bytes; other sizes run a kernel that takes 7 to 18 times as long.
+ *
+ * Routing to experts.  T tokens, E experts (at most MS_MAX_EXPERTS), K choices of each token.  ids, offsets and places are int32, weights and
+ * scales fp32.  Tensors need only be aligned to their elements; outputs are dense.  a_strides[1] = elements between rows of the first input (0 = dense).
+ *   ROUTE         dims T, E, K (at most MS_MAX_CHOSEN), groups (a divisor of E, at most MS_MAX_GROUPS), kept, best (1 or 2), flags (MS_ROUTE_*), the fp32 bits of
+ *                 a positive scale (0: 1).  F32, F16 or BF16 in, F32 out.  Inputs {X [T][E], bias fp32 [E] or NULL}, outputs {ids [T][K], W [T][K]}.
+ *                 Scores s = softmax(X[t]), or sigmoid(X[t]) with MS_ROUTE_SIGMOID.  Choice c = s + bias (has_bias 1) or s.  With groups > 1 (of E / groups neighbouring
+ *                 experts) the `kept` groups with the largest sums of their `best` largest c take part, a group with fewer experts to choose by those it has.
+ *                 ids[t] are the K experts with the largest c, in that order, the lower index first among equals; W their scores s, with
+ *                 MS_ROUTE_RENORMALISE over their sum (0 / 0 is NaN), times the scale.  c is computed in 64 bits and told apart down to 2^-41 of its size, so
+ *                 that a choice does not hang on how fp32 rounds; without a bias, and without groups or with best = 1, the logits themselves are compared.
+ *                 Experts whose logit is -infinity or NaN, or whose c is, cannot be chosen; where fewer than K can, the remaining ids are -1 and their weights 0.
+ *                 A NaN among a token's logits (softmax: or +infinity) makes all its weights NaN.
+ *   ROUTE_GRAD    dims T, E, K, flags, scale as above; out_dtype = in_dtype.  Inputs {X [T][E], ids [T][K], dW [T][K]}, output dX [T][E], written whole: the gradient
+ *                 of sum(W dW) for these ids, which need not be ROUTE's.  Ids outside [0, E) are no choices; one that occurs twice adds up.
+ *                 dX may be X itself where that is dense.
+ *   EXPERT_ORDER  dims E, T, K (T * K <= MS_MAX_CHOICES); I32 in and out, dense.  Input {ids [T][K]}, outputs {offsets [E + 1], place [T][K]}: the rows of expert e
+ *                 are those from offsets[e] up to offsets[e + 1], as GROUPED_GEMM takes them, one for each choice of e in the order of t and j;
+ *                 place = the row of a choice, -1 for ids outside [0, E).  Needs a workspace (ms_variant_info) for more than a few thousand choices.
+ *   SPREAD_ROWS   dims T, K (at most MS_MAX_ROW_CHOICES), N, P.  F32, F16 or BF16 in; out the same, I8 or F8E4M3; or I8 or F8E4M3 in and out.  Inputs {X [T][N], place [T][K],
+ *                 SX}, outputs {A [P][N], S}: A[place[t][j]] = X[t].  place may be NULL for K = 1 (P >= T): row t.  Into I8: S [P] = max(max |x| of the row times the fp32 number nearest to 1 / 127, 2^-126), A = x / S
+ *                 (the quotient in fp32) rounded to the nearest integer, ties to even.  Into F8E4M3: S [P][ceil(N / 128)] as RMS_NORM's, of x instead of y.  A NaN in a row
+ *                 (or block) makes its scale NaN, and 8-bit floats of the block.  8 bits in: S is the row of SX, [T] or [T][ceil(N / 128)].
+ *   JOIN_ROWS     dims T, K, N, P, weighted (0 or 1); F32, F16 or BF16 in, the same or F32 out.  Inputs {C [P][N], place [T][K], W [T][K] (weighted), R [T][N] of out_dtype (has_bias 1)},
+ *                 output Y [T][N] = R[t] + sum_j W[t][j] C[place[t][j]], summed in fp32 in the order of j.  R may be Y.  Unweighted it is the gradient of SPREAD_ROWS.
+ *   JOIN_GRAD     dims T, K, N, P; out_dtype = in_dtype.  Inputs {dY [T][N], place, W, C [P][N]}, outputs {dC [P][N], dW [T][K]}: dC[place[t][j]] = W[t][j] dY[t],
+ *                 dW[t][j] = sum_n dY[t][n] C[place[t][j]][n].  b_strides[1] = elements between rows of C (0 = N).
+ *   Places outside [0, P) are of no choice: they add nothing, dW is 0 there.  The others of a launch differ.  Rows of A and dC (and S) that no place
+ *   names are left as they were.  What these write lies apart from what they read, but for what is said above.
  */
 #define MS_EPS_UNIT 1e-12
+#define MS_MAX_CHOSEN 32
+#define MS_MAX_GROUPS 64
+#define MS_MAX_CHOICES (1 << 26)
+#define MS_MAX_ROW_CHOICES 64
+#define MS_ROUTE_SIGMOID 1
+#define MS_ROUTE_RENORMALISE 2
 #define MS_MAX_EXPERTS 1024
 #define MS_MAX_I8_DEPTH 131071 /* products of up to 2^14 in sums of 32 bits */
 #define MS_MAX_ROW_BYTES (4 << 20)
@@ -188,7 +229,7 @@ int32_t ms_op_loops(const ms_op *op, ms_loop *loops /* [MS_MAX_LOOPS] */, int32_
  * bytes = every input and output tensor moved once. */
 int32_t ms_op_work(const ms_op *op, double *flop, double *bytes);
 /* Byte size of input `idx` / of the output, for one instance. */
-int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx /* -1 = output; RMS_NORM: -2 = S, -3 = H */, int64_t *bytes);
+int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx /* -1 = output; RMS_NORM: -2 = S, -3 = H; routing: -2 = second output */, int64_t *bytes);
 
 /* ------------------------------------------------------------------ S(e0) */
 
@@ -263,7 +304,9 @@ typedef enum ms_slot_id {
                                  and the epilogue and need S = 1 */
     ,
     MS_SLOT_BLOCK = 14        /* categorical (layers of language models): what a workgroup works on.  0 = as the rules say, by the
-                                 operator's sizes.  Products: 1000 * rows + columns of its tile.  RMS_NORM: wavefronts that share a row */
+                                 operator's sizes.  Products: 1000 * rows + columns of its tile.  RMS_NORM: wavefronts that share a row.
+                                 ROUTE, ROUTE_GRAD: lanes that share a token.  EXPERT_ORDER: choices of a lane.  SPREAD_ROWS, JOIN_ROWS, JOIN_GRAD:
+                                 wavefronts that share a token */
 } ms_slot_id;
 
 /* Tensorize candidates: (m, n, k) of one matrix-core instruction.  The code
@@ -332,7 +375,8 @@ typedef struct ms_slot {
 
 typedef enum ms_family { MS_FAM_GEMM_ALU = 0, MS_FAM_GEMM_MFMA = 1, MS_FAM_DWCONV = 2,
                          MS_FAM_REDUCE = 3, /* softmax, norm: rows reduced by groups of lanes */
-                         MS_FAM_RMS_NORM = 4, MS_FAM_RAGGED = 5 /* SCALED_GEMM, GROUPED_GEMM, GROUPED_WGRAD */ } ms_family;
+                         MS_FAM_RMS_NORM = 4, MS_FAM_RAGGED = 5, /* SCALED_GEMM, GROUPED_GEMM, GROUPED_WGRAD */
+                         MS_FAM_ROUTING = 6 /* ROUTE to JOIN_GRAD */ } ms_family;
 
 typedef struct ms_space {
     int32_t family;
@@ -468,11 +512,14 @@ typedef enum ms_body {
     MS_BODY_RAGGED_TILES = 11, /* products over rows by expert: tiles whose operands lie in LDS; body_tile = 1000 * rows + columns */
     MS_BODY_RAGGED_PHASES = 13, /* the same in tiles of 256 x 256 under persistent workgroups whose wavefronts read and multiply in turn */
     MS_BODY_RAGGED_ROWS = 12,  /* the same of few rows for each expert: wavefronts of a workgroup share its reduction */
+    MS_BODY_ROUTE = 14,        /* ROUTE, ROUTE_GRAD: groups of lanes take a token; body_tile = lanes */
+    MS_BODY_ORDER = 15,        /* EXPERT_ORDER: runs of choices by workgroup; body_tile = choices of a lane */
+    MS_BODY_EXPERT_ROWS = 16,  /* SPREAD_ROWS, JOIN_ROWS, JOIN_GRAD; body_tile = wavefronts that share a token */
     MS_BODY_FEW_ROWS = 9     /* the same of a nest over up to 128 rows times a row-major matrix (fp16, bf16), of launches of up to 64 x 64
                                 outputs per compute unit: wavefronts of a workgroup share its reduction; body_tile packs the tile */
 } ms_body;
 
-/* Bodies 10 to 13 are those of the layers of language models, whose kernels take sizes as arguments. */
+/* Bodies 10 to 16 are those of the layers of language models, whose kernels take sizes as arguments. */
 
 /* What the trace interpreter derives.  Unused fields are zero.  With bodies 1 to 3 and 6, block_*, grid, threads,
  * waves, acc_per_thread, lds_bytes, vec and vec_b are those of the kernel that runs, and so are the splits ti, tj, tc and tk
@@ -541,7 +588,7 @@ typedef struct ms_variant ms_variant;
 int32_t ms_variant_build(const ms_op *op, const ms_space *space, const ms_trace *trace, ms_variant **out);
 void ms_variant_destroy(ms_variant *v);
 /* params and workspace_bytes may be NULL.  *workspace_bytes = bytes of workspace ONE instance needs (0 unless
- * rfactor > 1: rfactor x batch x M x N accumulator values); a launch over R instances needs R times as much. */
+ * rfactor > 1: rfactor x batch x M x N accumulator values; or of EXPERT_ORDER where it has several runs: their counts); a launch over R instances needs R times as much. */
 int32_t ms_variant_info(const ms_variant *v, ms_variant_params *params, size_t *workspace_bytes);
 /* What a launch over `instances` instances runs: the body's tile, workgroups per instance, bytes of LDS of a workgroup.  They
  * are the fields of ms_variant_params unless the variant has a kernel of its own for many instances (body_tile_many), for
@@ -583,7 +630,7 @@ int32_t ms_jit_stats(int64_t *compiled, int64_t *from_disk, int64_t *from_memory
 
 /* Enqueue one execution over `instances` instances on `stream`.  inputs /
  * outputs: host arrays of device pointers (see ms_op_desc for the order; one
- * output, RMS_NORM three, NULL where it has none).  16-byte aligned pointers are always enough; the kernels of MS_BODY_ROW_VECTORS, MS_BODY_STRIPS and
+ * output, RMS_NORM three, routing up to two, NULL where it has none).  16-byte aligned pointers are always enough; the kernels of MS_BODY_ROW_VECTORS, MS_BODY_STRIPS and
  * MS_BODY_IMAGE_ROWS need tensors aligned to their elements only (the bias to 16 bytes).  workspace: device pointer, 16-byte aligned, of at least instances x
  * workspace_bytes (ms_variant_info), owned by the caller and not shared with a
  * launch that may run at the same time; NULL if that is 0.  Its contents need no

@@ -13,7 +13,8 @@ LIB_PATH = os.path.join(HERE, "libms.so")
 
 MS_OK, MS_ERR_BAD_ARG, MS_ERR_INVALID_TRACE, MS_ERR_UNSUPPORTED, MS_ERR_COMPILE, MS_ERR_HIP, MS_ERR_NOMEM = range(7)
 (OP_GEMM, OP_BMM_NT, OP_BMM_NN, OP_CONV2D_NHWC, OP_DWCONV2D_NHWC, OP_SOFTMAX, OP_NORM,
- OP_CONV2D_TRANSPOSED_NHWC, OP_CONV1D_NWC, OP_CONV3D_NDHWC, OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD) = range(14)
+ OP_CONV2D_TRANSPOSED_NHWC, OP_CONV1D_NWC, OP_CONV3D_NDHWC, OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD,
+ OP_ROUTE, OP_ROUTE_GRAD, OP_EXPERT_ORDER, OP_SPREAD_ROWS, OP_JOIN_ROWS, OP_JOIN_GRAD) = range(20)
 F32, F16, BF16, I8, I32 = range(5)
 SLOT_PERFECT_TILE, SLOT_CATEGORICAL = 0, 1
 (SLOT_TENSORIZE, SLOT_TILE_I, SLOT_TILE_J, SLOT_TILE_C, SLOT_TILE_K, SLOT_UNROLL, SLOT_CACHE_READ, SLOT_VECTORIZE,
@@ -25,11 +26,14 @@ SPACE_TAP_ROWS = 0x200  # opt-in: conv2d reduction laid out as filter rows (firs
 SPACE_RFACTOR = 0x400  # opt-in: sample the split of the reduction across workgroups (needs a workspace)
 SPACE_DEFAULT = 0xFF
 STATIC_WORKSPACE_BYTES = 32 << 20
-FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE, FAM_RMS_NORM, FAM_RAGGED = range(6)
+FAM_GEMM_ALU, FAM_GEMM_MFMA, FAM_DWCONV, FAM_REDUCE, FAM_RMS_NORM, FAM_RAGGED, FAM_ROUTING = range(7)
 (BODY_NEST, BODY_ROW_VECTORS, BODY_STRIPS, BODY_IMAGE_ROWS, BODY_PHASES, BODY_DOUBLE_STEPS, BODY_CONV_STEPS, BODY_CONV_PATCH, BODY_CONV_PLANES,
- BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS, BODY_RAGGED_PHASES) = range(14)
+ BODY_FEW_ROWS, BODY_RMS_ROWS, BODY_RAGGED_TILES, BODY_RAGGED_ROWS, BODY_RAGGED_PHASES,
+ BODY_ROUTE, BODY_ORDER, BODY_EXPERT_ROWS) = range(17)
 EPS_UNIT, MAX_EXPERTS, MAX_I8_DEPTH, SCALE_BLOCK = 1e-12, 1024, 131071, 128
-LAYERS = (OP_RMS_NORM, OP_SCALED_GEMM, OP_GROUPED_GEMM, OP_GROUPED_WGRAD)
+MAX_CHOSEN, MAX_GROUPS, MAX_CHOICES, MAX_ROW_CHOICES = 32, 64, 1 << 26, 64
+ROUTE_SIGMOID, ROUTE_RENORMALISE = 1, 2
+LAYERS = tuple(range(OP_RMS_NORM, OP_JOIN_GRAD + 1))
 MAX_SLOTS, MAX_FACTORS, MAX_CANDS, MAX_LOOPS = 16, 4, 12, 8
 
 F8E4M3 = 5
@@ -386,6 +390,49 @@ def grouped_gemm_op(E, T, N, K, rows_of_k=True, in_dtype="bf16", out_dtype=None,
 def grouped_wgrad_op(E, T, I, J, in_dtype="bf16", out_dtype=None, **kw):
     """D [E, I, J]: of each expert the sum of P[t, i] Q[t, j] over its rows t of P [T, I], Q [T, J]; inputs (P, Q, offsets int32 [E + 1])."""
     return Op(OP_GROUPED_WGRAD, in_dtype, out_dtype or in_dtype, [E, T, I, J], **kw)
+
+
+# ---- routing to experts, around the products by expert
+def _route_flags(scores, renormalise, scale):
+    import struct
+    if scores not in ("softmax", "sigmoid"):
+        raise ValueError("scores = %r" % (scores,))
+    if not 2.0 ** -126 <= scale < 2.0 ** 128:
+        raise ValueError("scale = %r" % (scale,))
+    return [(ROUTE_SIGMOID if scores == "sigmoid" else 0) | (ROUTE_RENORMALISE if renormalise else 0), struct.unpack("<I", struct.pack("<f", scale))[0]]
+
+
+def route_op(T, E, K, in_dtype="f32", scores="softmax", bias=False, groups=1, kept=1, best=1, renormalise=False, scale=1.0, **kw):
+    """The K of E experts that each token goes to and their weights; inputs (X [T, E], bias fp32 [E] or None), outputs (ids int32 [T, K], W fp32 [T, K]).
+    groups: of neighbouring experts, the `kept` with the largest sums of their `best` largest choices take part.  scale is rounded to fp32."""
+    return Op(OP_ROUTE, in_dtype, "f32", [T, E, K, groups, kept, best] + _route_flags(scores, renormalise, scale), has_bias=bias, **kw)
+
+
+def route_grad_op(T, E, K, in_dtype="f32", scores="softmax", renormalise=False, scale=1.0, **kw):
+    """The gradient of route_op's logits: inputs (X [T, E], ids int32 [T, K], dW fp32 [T, K]), output dX [T, E]."""
+    return Op(OP_ROUTE_GRAD, in_dtype, in_dtype, [T, E, K] + _route_flags(scores, renormalise, scale), **kw)
+
+
+def expert_order_op(E, T, K):
+    """The choices sorted by expert: input ids int32 [T, K], outputs (offsets int32 [E + 1], place int32 [T, K]); Variant.workspace_bytes() says what it
+    needs beside them."""
+    return Op(OP_EXPERT_ORDER, "i32", "i32", [E, T, K])
+
+
+def spread_rows_op(T, K, N, P, in_dtype="bf16", out_dtype=None, **kw):
+    """A [P, N]: row place[t, j] is X[t], quantised for out_dtype "i8" (scales S [P]) or "f8" (S [P, ceil(N / 128)]); inputs (X [T, N], place int32 [T, K] or, for K = 1,
+    None, for 8 bits in their scales), outputs (A, S or None)."""
+    return Op(OP_SPREAD_ROWS, in_dtype, out_dtype or in_dtype, [T, K, N, P], **kw)
+
+
+def join_rows_op(T, K, N, P, in_dtype="bf16", out_dtype=None, weights=True, residual=False, **kw):
+    """Y [T, N]: R[t] + sum over j of W[t, j] C[place[t, j]]; inputs (C [P, N], place int32 [T, K], W fp32 [T, K] or None, R [T, N] or None)."""
+    return Op(OP_JOIN_ROWS, in_dtype, out_dtype or in_dtype, [T, K, N, P, int(weights)], has_bias=residual, **kw)
+
+
+def join_grad_op(T, K, N, P, in_dtype="bf16", **kw):
+    """The gradients of join_rows_op's C and W: inputs (dY [T, N], place, W, C [P, N]), outputs (dC [P, N], dW fp32 [T, K])."""
+    return Op(OP_JOIN_GRAD, in_dtype, in_dtype, [T, K, N, P], **kw)
 
 
 MAX_MODULES = 16

@@ -2,6 +2,7 @@
 // trace sampling / mutation / text form, trace interpreter and validator.
 // Nothing in this file touches the GPU.
 #include "ms_internal.h"
+#include "ms_routing.h"
 
 #include <algorithm>
 #include <cinttypes>
@@ -117,6 +118,12 @@ const char *op_kind_name(int32_t kind)
     case MS_OP_SCALED_GEMM: return "scaled_gemm";
     case MS_OP_GROUPED_GEMM: return "grouped_gemm";
     case MS_OP_GROUPED_WGRAD: return "grouped_wgrad";
+    case MS_OP_ROUTE: return "route";
+    case MS_OP_ROUTE_GRAD: return "route_grad";
+    case MS_OP_EXPERT_ORDER: return "expert_order";
+    case MS_OP_SPREAD_ROWS: return "spread_rows";
+    case MS_OP_JOIN_ROWS: return "join_rows";
+    case MS_OP_JOIN_GRAD: return "join_grad";
     default: return "?";
     }
 }
@@ -188,6 +195,7 @@ static int64_t conv_out(int64_t in, int64_t k, int64_t s, int64_t p)
 // Layers of language models: the operator in *op, its dims and types checked.
 static int32_t create_layer(const ms_op_desc &d, ms_op *op)
 {
+    if (is_routing(d.kind)) return create_routing(d, op);
     const int ndims = d.kind == MS_OP_RMS_NORM || d.kind == MS_OP_SCALED_GEMM ? 3 : 4;
     for (int i = 0; i < ndims; ++i) {
         const bool eps = d.kind == MS_OP_RMS_NORM && i == 2; // may be zero, and any number of units up to 1
@@ -486,6 +494,13 @@ extern "C" int32_t ms_op_loops(const ms_op *op, ms_loop *loops, int32_t *n_loops
         set_loop(&loops[n++], "k", op->K, 1);
         break;
     }
+    if (is_routing(op->d.kind)) {
+        set_loop(&loops[n++], "i", op->M, 0); // tokens
+        if (op->d.kind == MS_OP_EXPERT_ORDER) set_loop(&loops[n++], "j", op->N, 1); // choices: compared with those ahead of them
+        else set_loop(&loops[n++], "j", is_route(op->d.kind) ? op->N : op->K, op->d.kind == MS_OP_JOIN_ROWS);
+        if (is_route(op->d.kind)) set_loop(&loops[n++], "k", op->K, 1); // experts
+        else if (moves_rows(op->d.kind)) set_loop(&loops[n++], "k", op->N, op->d.kind == MS_OP_JOIN_GRAD); // columns
+    }
     *n_loops = n;
     return MS_OK;
 }
@@ -494,6 +509,12 @@ extern "C" int32_t ms_op_tensor_bytes(const ms_op *op, int32_t idx, int64_t *byt
 {
     if (!op || !bytes) return fail(MS_ERR_BAD_ARG, "ms_op_tensor_bytes: NULL argument");
     const ms_op_desc &d = op->d;
+    if (is_routing(d.kind)) {
+        const int64_t n = routing_tensor_bytes(op, idx);
+        if (n < 0) return fail(MS_ERR_BAD_ARG, "ms_op_tensor_bytes: no tensor %d", idx);
+        *bytes = n;
+        return MS_OK;
+    }
     int64_t e = -1;
     int sz = idx < 0 ? op->out_size : op->in_size;
     switch (d.kind) {
@@ -562,6 +583,7 @@ extern "C" int32_t ms_op_work(const ms_op *op, double *flop, double *bytes)
     if (!op || !flop || !bytes) return fail(MS_ERR_BAD_ARG, "ms_op_work: NULL argument");
     const ms_op_desc &d = op->d;
     double f = 0, b = 0;
+    if (is_routing(d.kind)) routing_work(op, &f, &b);
     switch (d.kind) {
     case MS_OP_GEMM:
     case MS_OP_BMM_NT:
@@ -659,8 +681,10 @@ extern "C" int32_t ms_space_describe(const ms_op *op, uint32_t flags, ms_space *
     memset(out, 0, sizeof *out);
     const ms_op_desc &d = op->d;
     if (is_layer(d.kind)) { // no module changes their kernels; the one decision is what a workgroup works on
-        out->family = d.kind == MS_OP_RMS_NORM ? MS_FAM_RMS_NORM : MS_FAM_RAGGED;
-        if (d.kind == MS_OP_RMS_NORM) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
+        out->family = layer_family(d.kind);
+        if (is_route(d.kind)) add_cat(out, MS_SLOT_BLOCK, "block", {0, 8, 16, 32, 64});
+        else if (is_routing(d.kind)) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
+        else if (d.kind == MS_OP_RMS_NORM) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
         else add_cat(out, MS_SLOT_BLOCK, "block", {0, 16016, 16032, 32032, 64032, 64128, 128128, 256256});
         ms_slot &s = out->slots[0];
         for (int c = 1; c < s.n_candidates; ++c)
@@ -1207,7 +1231,10 @@ extern "C" int32_t ms_trace_to_text(const ms_op *op, const ms_space *space, cons
         if (p.body == MS_BODY_CONV_STEPS) appendf(s, "# body=conv-steps: %d pixels x %d channels per workgroup, this operator's own split\n", p.block_m, p.block_n);
         if (p.body == MS_BODY_DOUBLE_STEPS) appendf(s, "# body=double-steps: two k0 steps per LDS stage, %d stages\n", p.body_tile);
         if (is_layer_family(p.family)) {
-            if (p.body == MS_BODY_RMS_ROWS) appendf(s, "# body=rms-rows: %d wavefronts share a row, which stays in their registers\n", p.body_tile);
+            if (p.body == MS_BODY_ROUTE) appendf(s, "# body=route: %d lanes share a token, %d experts at most\n", p.body_tile, p.block_k);
+            else if (p.body == MS_BODY_ORDER) appendf(s, "# body=order: runs of %d choices\n", p.block_m);
+            else if (p.body == MS_BODY_EXPERT_ROWS) appendf(s, "# body=rows: %d wavefronts share a token\n", p.body_tile);
+            else if (p.body == MS_BODY_RMS_ROWS) appendf(s, "# body=rms-rows: %d wavefronts share a row, which stays in their registers\n", p.body_tile);
             else appendf(s, "# body=%s: %d rows of one expert x %d columns per workgroup, the last of each masked\n",
                          p.body == MS_BODY_RAGGED_ROWS ? "ragged-rows" : p.body == MS_BODY_RAGGED_PHASES ? "ragged-phases" : "ragged-tiles", p.block_m, p.block_n);
             appendf(s, "# sizes are arguments of the kernel; workgroup=%d threads, grid=%d, lds=%d B\n", p.threads, p.grid[0], p.lds_bytes);

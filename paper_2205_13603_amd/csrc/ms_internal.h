@@ -31,8 +31,10 @@ inline bool follows_decisions(const ms_variant_params *p)
     return p->body == MS_BODY_NEST || p->body == MS_BODY_PHASES || p->body == MS_BODY_DOUBLE_STEPS;
 }
 // Layers of language models: sizes are arguments of their kernels
-inline bool is_layer(int32_t kind) { return kind >= MS_OP_RMS_NORM && kind <= MS_OP_GROUPED_WGRAD; }
-inline bool is_layer_family(int32_t family) { return family == MS_FAM_RMS_NORM || family == MS_FAM_RAGGED; }
+inline bool is_layer(int32_t kind) { return kind >= MS_OP_RMS_NORM && kind <= MS_OP_JOIN_GRAD; }
+inline bool is_routing(int32_t kind) { return kind >= MS_OP_ROUTE && kind <= MS_OP_JOIN_GRAD; } // ms_routing.h
+inline int32_t layer_family(int32_t kind) { return is_routing(kind) ? MS_FAM_ROUTING : kind == MS_OP_RMS_NORM ? MS_FAM_RMS_NORM : MS_FAM_RAGGED; }
+inline bool is_layer_family(int32_t family) { return family == MS_FAM_RMS_NORM || family == MS_FAM_RAGGED || family == MS_FAM_ROUTING; }
 // products whose operands come with scales: for blocks of 128 k values, of 8-bit integers for rows and columns
 inline bool has_scales(const ms_op_desc &d) { return d.in_dtype == MS_F8E4M3 || d.in_dtype == MS_I8; }
 inline int64_t scale_blocks(int64_t n) { return (n + 127) / 128; }
@@ -96,6 +98,7 @@ struct KernelSpec {
     std::string template_name; // file in kernels/
     std::vector<std::string> defines;
     std::string entry;         // kernel symbol
+    std::string first;         // of a layer: the kernel that a launch runs ahead of it, if any
     unsigned block[3];
     unsigned grid[3];          // per instance; instances multiply grid[2]
     unsigned lds_dynamic;

@@ -5,6 +5,7 @@
 // Host only.
 #include "kernels/ragged_schedule.h"
 #include "ms_internal.h"
+#include "ms_routing.h"
 
 #include <algorithm>
 #include <cinttypes>
@@ -822,13 +823,16 @@ int64_t rms_rule(const ms_op *op)
 int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *trace, ms_variant_params *p)
 {
     int64_t code = cat_value(space, trace, MS_SLOT_BLOCK, 0);
-    if (space->family != (op->d.kind == MS_OP_RMS_NORM ? MS_FAM_RMS_NORM : MS_FAM_RAGGED)) return fail(MS_ERR_BAD_ARG, "ms_trace_validate: the space is another operator's");
+    if (space->family != layer_family(op->d.kind)) return fail(MS_ERR_BAD_ARG, "ms_trace_validate: the space is another operator's");
     if (code && !layer_block_fits(op, code)) return reject("block: this operator has no kernel for %" PRId64, code);
     p->grid[1] = p->grid[2] = 1;
     p->rfactor = 1;
     p->tile_unit[0] = p->tile_unit[1] = p->tile_unit[2] = 1;
     int64_t grid;
-    if (op->d.kind == MS_OP_RMS_NORM) {
+    if (is_routing(op->d.kind)) {
+        if (!code) code = routing_rule(op);
+        resolve_routing(op, code, p, &grid);
+    } else if (op->d.kind == MS_OP_RMS_NORM) {
         if (!code) code = rms_rule(op);
         p->body = MS_BODY_RMS_ROWS;
         p->waves = std::max(4, (int)code);
@@ -882,6 +886,10 @@ uint64_t hash_params(const ms_op *op, const ms_variant_params *p)
         add((uint64_t)p->vec);
         add((uint64_t)p->threads);
         add((uint64_t)p->lds_bytes);
+        if (is_routing(d.kind)) {
+            std::vector<std::string> D;
+            (void)routing_spec(op, p, D, [&](const char *, int64_t v) { return add((uint64_t)v), std::string(); });
+        }
         return h;
     }
     add((uint64_t)d.kind);
@@ -1515,6 +1523,7 @@ int32_t ms::validate_as_nest(const ms_op *op, const ms_space *space, const ms_tr
 
 bool ms::layer_block_fits(const ms_op *op, int64_t code)
 {
+    if (is_routing(op->d.kind)) return routing_block_fits(op, code);
     if (op->d.kind == MS_OP_RMS_NORM) return code >= 1 && code <= 16 && (code & (code - 1)) == 0;
     const bool few = code % 1000 <= 32;
     if (!ragged_aligned(op)) return code == 64128;
@@ -1574,6 +1583,12 @@ int32_t make_kernel_spec(const ms_op *op, const ms_variant_params *p, KernelSpec
     auto &D = k.defines;
     D.push_back(def("IN_DT", dt_code(d.in_dtype)));
     D.push_back(def("OUT_DT", dt_code(d.out_dtype)));
+    if (p->family == MS_FAM_ROUTING) {
+        k.template_name = routing_spec(op, p, D, def);
+        if (p->body == MS_BODY_ORDER && p->grid[0] > 1) k.first = "ms_count";
+        *out = k;
+        return MS_OK;
+    }
     if (p->family == MS_FAM_RMS_NORM) {
         D.push_back(def("WAVES", p->body_tile));
         D.push_back(def("RESIDUAL", d.has_bias));
@@ -1831,7 +1846,8 @@ static inline int64_t split_index(const int32_t *f, int64_t x0, int64_t x1, int6
 
 static bool layer_params_fit(const ms_op *op, const ms_variant_params *p)
 {
-    if (!is_layer(op->d.kind) || (op->d.kind == MS_OP_RMS_NORM) != (p->family == MS_FAM_RMS_NORM)) return false;
+    if (!is_layer(op->d.kind) || layer_family(op->d.kind) != p->family) return false;
+    if (is_routing(op->d.kind)) return routing_block_fits(op, p->body_tile) && p->grid[0] > 0 && p->block_m > 0 && p->vec > 0;
     return layer_block_fits(op, p->body_tile) && p->grid[0] > 0 && p->block_k > 0 && p->threads >= (op->d.kind == MS_OP_RMS_NORM ? 64 * p->body_tile : 64);
 }
 
@@ -1942,7 +1958,8 @@ extern "C" int32_t ms_variant_coverage(const ms_op *op, const ms_variant_params 
     const ms_op_desc &d = op->d;
     if (is_layer_family(p->family)) {
         if (!layer_params_fit(op, p)) return fail(MS_ERR_BAD_ARG, "ms_variant_coverage: the parameters are another operator's");
-        if (p->family == MS_FAM_RMS_NORM) rms_coverage(op, p, counts);
+        if (p->family == MS_FAM_ROUTING) routing_coverage(op, p, counts);
+        else if (p->family == MS_FAM_RMS_NORM) rms_coverage(op, p, counts);
         else ragged_coverage(op, p, counts);
         return MS_OK;
     }
@@ -2070,11 +2087,13 @@ extern "C" int32_t ms_variant_reduction_coverage(const ms_op *op, const ms_varia
     if (!op || !p) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
     if (is_layer_family(p->family)) {
         if (!layer_params_fit(op, p)) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: the parameters are another operator's");
-        if (needed) *needed = op->K;
+        const int64_t length = is_routing(op->d.kind) ? routing_reduction(op) : op->K;
+        if (needed) *needed = length;
         if (!counts) return needed ? MS_OK : fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: NULL argument");
-        if (k_elems != op->K) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: k_elems %" PRId64 " != %" PRId64, k_elems, op->K);
+        if (k_elems != length) return fail(MS_ERR_BAD_ARG, "ms_variant_reduction_coverage: k_elems %" PRId64 " != %" PRId64, k_elems, length);
         memset(counts, 0, sizeof(int32_t) * (size_t)k_elems);
-        if (p->family == MS_FAM_RMS_NORM) rms_columns(op, p, [&](int64_t k) { ++counts[k]; });
+        if (p->family == MS_FAM_ROUTING) routing_reduction_coverage(op, p, counts);
+        else if (p->family == MS_FAM_RMS_NORM) rms_columns(op, p, [&](int64_t k) { ++counts[k]; });
         else ragged_reduction(op, p, counts);
         return MS_OK;
     }

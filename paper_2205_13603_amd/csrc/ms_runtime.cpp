@@ -1,6 +1,7 @@
 // Variant handles, launch and measurement (the only part of libms that talks
 // to the GPU).
 #include "ms_internal.h"
+#include "ms_routing.h"
 
 #include <hip/hip_runtime.h>
 
@@ -103,9 +104,10 @@ extern "C" void ms_variant_destroy(ms_variant *v)
     delete v;
 }
 
-// rfactor partial results of one instance: [rfactor][batch][M][N] accumulator values (fp32 or int32)
+// rfactor partial results of one instance: [rfactor][batch][M][N] accumulator values (fp32 or int32); of EXPERT_ORDER the counts of its runs
 static size_t workspace_per_instance(const ms_variant *v)
 {
+    if (is_routing(v->op.d.kind)) return routing_workspace(&v->op, &v->p);
     if (v->p.rfactor <= 1) return 0;
     return (size_t)v->p.rfactor * (size_t)v->op.nb * (size_t)v->op.M * (size_t)v->op.N * 4u;
 }
@@ -282,7 +284,7 @@ static int32_t ensure_loaded(ms_variant *v, int dev)
 // devices and threads at once: what it points to never changes.
 struct LoadedKernel {
     hipModule_t mod;
-    hipFunction_t fn;
+    hipFunction_t fn, first; // first: runs ahead of fn, null if there is none
     int device, compute_units;
 };
 static std::mutex g_layers_mu;
@@ -312,9 +314,10 @@ static int32_t load_layer(ms_variant *v, int dev, const LoadedKernel **loaded)
     {
         std::lock_guard<std::mutex> lk(g_layers_mu);
         if (g_layers.find({v->code, dev}) == g_layers.end()) { // no other thread was quicker
-            LoadedKernel k = {nullptr, nullptr, dev, prop.multiProcessorCount};
+            LoadedKernel k = {nullptr, nullptr, nullptr, dev, prop.multiProcessorCount};
             HIP_TRY(hipModuleLoadData(&k.mod, v->code->data()));
-            const hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
+            hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
+            if (e == hipSuccess && !v->spec.first.empty()) e = hipModuleGetFunction(&k.first, k.mod, v->spec.first.c_str());
             bool kept = e == hipSuccess;
             try {
                 if (kept) g_layers.emplace(std::make_pair(v->code, dev), k);
@@ -347,10 +350,82 @@ static bool layer_has_output(const ms_op &op, int i)
     return i == 0 || (op.d.kind == MS_OP_RMS_NORM && (i == 1 ? op.d.out_dtype == MS_F8E4M3 : i == 2 && op.d.has_bias));
 }
 
-static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *const *outputs, int32_t instances, void *stream)
+// The same of routing's operators: their kernels' arguments from the tensors of a launch, which are checked.
+static int32_t launch_routing(ms_variant *v, const void *const *inputs, void *const *outputs, void *workspace, int32_t instances, void *stream)
 {
     const ms_op &op = v->op;
     const ms_op_desc &d = op.d;
+    const void *in[4] = {nullptr, nullptr, nullptr, nullptr};
+    void *out[2] = {nullptr, nullptr};
+    // place may be NULL where a token has one choice: its row is the token's own
+    const bool own_rows = d.kind == MS_OP_SPREAD_ROWS && op.K == 1 && !inputs[1];
+    for (int i = 0; i < routing_inputs(d.kind); ++i) {
+        if (routing_tensor_bytes(&op, i) < 0 || (i == 1 && own_rows)) continue;
+        in[i] = inputs[i];
+        if (!in[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: inputs[%d] of %s is NULL", i, op_kind_name(d.kind));
+    }
+    for (int i = 0; i < routing_outputs(d.kind); ++i) {
+        if (routing_tensor_bytes(&op, -1 - i) <= 0) continue;
+        out[i] = outputs[i];
+        if (!out[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: outputs[%d] of %s is NULL", i, op_kind_name(d.kind));
+    }
+    if (instances > 65535) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %d instances overflow the grid", instances);
+    const bool rows = moves_rows(d.kind), ids = d.kind == MS_OP_ROUTE || d.kind == MS_OP_EXPERT_ORDER;
+    auto aligned = [](const void *p, int64_t to) { return ((uintptr_t)p & (uintptr_t)(to - 1)) == 0; };
+    for (int i = 0; i < 4; ++i) {
+        const int64_t to = i == 0 ? op.in_size : i == 3 ? (d.kind == MS_OP_JOIN_ROWS ? op.out_size : op.in_size) : 4;
+        if (!aligned(in[i], to)) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: inputs[%d] of %s is not aligned to its elements", i, op_kind_name(d.kind));
+    }
+    if (!aligned(out[0], ids ? 4 : op.out_size) || !aligned(out[1], 4)) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: an output of %s is not aligned to its elements", op_kind_name(d.kind));
+    // other tokens' rows would be written over ones that are still to be read
+    if ((rows && (out[0] == in[0] || (d.kind == MS_OP_JOIN_GRAD && out[0] == in[3]))) || (d.kind == MS_OP_ROUTE_GRAD && out[0] == in[0] && op.M > 1 && d.a_strides[1] != op.K))
+        return fail(MS_ERR_BAD_ARG, "ms_variant_launch: the output of %s cannot lie where its input does", op_kind_name(d.kind));
+    if (own_rows && moved_rows(&op) < op.M) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %s without places needs a row for each token", op_kind_name(d.kind));
+    const size_t need = routing_workspace(&op, &v->p);
+    if (need && (!workspace || !aligned(workspace, 16))) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: %s needs a workspace of %zu bytes per instance, 16-byte aligned", op_kind_name(d.kind), need);
+
+    const int64_t span = routing_tensor_bytes(&op, 0), a = d.a_strides[1];
+    RouteArgs route;
+    RouteGradArgs grad;
+    OrderArgs order;
+    RowsArgs moved;
+    void *args[1];
+    switch (d.kind) {
+    case MS_OP_ROUTE:
+        route = {in[0], in[1], out[0], out[1], a, span / op.in_size, (int32_t)op.M, (int32_t)op.K, (int32_t)op.N, (int32_t)d.dims[3], (int32_t)d.dims[4], route_scale(d)};
+        args[0] = &route;
+        break;
+    case MS_OP_ROUTE_GRAD:
+        grad = {in[0], in[1], in[2], out[0], a, span / op.in_size, (int32_t)op.M, (int32_t)op.K, (int32_t)op.N, route_scale(d)};
+        args[0] = &grad;
+        break;
+    case MS_OP_EXPERT_ORDER:
+        order = {in[0], out[0], out[1], workspace, (int32_t)(op.M * op.N), (int32_t)op.K, v->p.grid[0]};
+        args[0] = &order;
+        break;
+    default: {
+        // the tensor beside X: scales, residual, or rows of C
+        const bool grads = d.kind == MS_OP_JOIN_GRAD, spread = d.kind == MS_OP_SPREAD_ROWS;
+        moved = {in[0], in[1], spread ? nullptr : in[2], spread ? in[2] : in[3], out[0], (void *)out[1], a * op.in_size, span, 0, 0, (int32_t)op.M, (int32_t)op.K, (int32_t)op.N, (int32_t)moved_rows(&op)};
+        if (grads) moved.c_row = d.b_strides[1] * op.in_size, moved.c_inst = routing_tensor_bytes(&op, 3);
+        args[0] = &moved;
+    }
+    }
+    int dev = 0;
+    HIP_TRY(hipGetDevice(&dev));
+    const LoadedKernel *kernel;
+    const int32_t rc = load_layer(v, dev, &kernel);
+    if (rc != MS_OK) return rc;
+    for (hipFunction_t fn : {kernel->first, kernel->fn}) // stream order makes the first one's counts visible to the second
+        if (fn) HIP_TRY(hipModuleLaunchKernel(fn, v->spec.grid[0], (unsigned)instances, 1, v->spec.block[0], 1, 1, 0, (hipStream_t)stream, args, nullptr));
+    return MS_OK;
+}
+
+static int32_t launch_layer(ms_variant *v, const void *const *inputs, void *const *outputs, void *workspace, int32_t instances, void *stream)
+{
+    const ms_op &op = v->op;
+    const ms_op_desc &d = op.d;
+    if (is_routing(d.kind)) return launch_routing(v, inputs, outputs, workspace, instances, stream);
     const int ni = layer_inputs(op);
     for (int i = 0; i < ni; ++i)
         if (!inputs[i]) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: inputs[%d] of %s is NULL", i, d.kind == MS_OP_RMS_NORM ? "the norm" : "the product");
@@ -526,7 +601,7 @@ extern "C" int32_t ms_variant_launch(ms_variant *v, const void *const *inputs, v
 {
     if (!v || !inputs || !outputs) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: NULL argument");
     if (instances < 1) return fail(MS_ERR_BAD_ARG, "ms_variant_launch: instances = %d", instances);
-    if (is_layer_family(v->p.family)) return launch_layer(v, inputs, outputs, instances, stream);
+    if (is_layer_family(v->p.family)) return launch_layer(v, inputs, outputs, workspace, instances, stream);
     if (v->p.rfactor > 1 && !workspace)
         return fail(MS_ERR_BAD_ARG, "ms_variant_launch: the variant splits its reduction over %d workgroups and needs a workspace of %zu bytes per instance",
                     v->p.rfactor, workspace_per_instance(v));
@@ -662,7 +737,9 @@ extern "C" int32_t ms_measure(ms_variant *v, const ms_bufset *sets, int32_t n_se
                 return p ? (char *)p + (bytes * cfg->instances + 255) / 256 * 256 : nullptr;
             };
             void *outs[3] = {b.output, nullptr, nullptr};
-            if (v->op.d.kind == MS_OP_RMS_NORM) {
+            if (is_routing(v->op.d.kind)) {
+                if (routing_outputs(v->op.d.kind) == 2) outs[1] = next(outs[0], -1);
+            } else if (v->op.d.kind == MS_OP_RMS_NORM) {
                 outs[1] = next(outs[0], -1);
                 outs[2] = next(outs[1], -2);
             }
