@@ -6,8 +6,8 @@
 //   GRAD   Y[place[t][j]] = W[t][j] X[t], S[t][j] = sum_c X[t][c] C[place[t][j]][c]: the gradients of BACK's X and W where X here is that of its Y
 // Places outside of [0, rows) are of no choice: nothing is read or written for them, S is 0 there.
 //
-// WAVES wavefronts share a token, 8 neighbouring columns of a lane in each chunk of 512 columns; OUT and GRAD keep up to NV chunks in registers and
-// read what lies beyond again.  A token's places and weights lie in the lanes of each of its wavefronts, from where scalar registers take them: a row's
+// WAVES wavefronts share a token, 8 neighbouring columns of a lane in each chunk of 512 columns; OUT keeps up to NV chunks in registers and reads what
+// lies beyond again.  A token's places and weights lie in the lanes of each of its wavefronts, from where scalar registers take them: a row's
 // address is computed once, by the scalar unit.
 #include "common.h"
 #include "rows.h"
@@ -23,7 +23,7 @@ struct rows_args {
     int tokens, chosen, cols, rows;
 };
 
-constexpr int NV = 4, THREADS = WAVES < 4 ? 256 : WAVES * 64, GROUPS = THREADS / 64 / WAVES, STEP = WAVES * 512;
+constexpr int NV = 4, THREADS = WAVES < 3 ? 256 : WAVES * 64, GROUPS = THREADS / 64 / WAVES, STEP = WAVES * 512;
 constexpr int OUT = 0, BACK = 1, GRAD = 2, ES = sizeof(in_t), OS = sizeof(out_t);
 constexpr bool BYTES = ES == 1, TO_I8 = OUT_DT == DT_I8 && !BYTES, TO_F8 = OUT_DT == DT_F8E4M3 && !BYTES;
 
@@ -107,6 +107,12 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
     const int cols = live ? g.cols : 0, chosen = live ? g.chosen : 0, c0 = (part * 64 + lane) * 8;
     const long at = (long)inst * g.tokens + (live ? token : 0);
 
+    // A lane's eight columns.  The last ones of a row begin eight ahead of its end and share some with the lane before, which has the same values:
+    // no load or store is one of single columns.  Rows of less than eight columns: one by one.
+    const bool wide = g.cols >= 8;
+    auto begin = [&](int c) { return wide && c > g.cols - 8 ? g.cols - 8 : c; };
+    auto left = [&](int c) { return wide ? 8 : g.cols - c; }; // of them that there are
+
     // ---- the token's choices: place j in lane j, -1 where it is none
     int place = -1;
     float weight = 1;
@@ -116,6 +122,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
         if (MODE != OUT && g.w) weight = g.w[at * g.chosen + lane];
     }
     const unsigned long real = __ballot(place >= 0);
+    auto take = [&](const char *row, int c) { return take8(row + (long)begin(c) * ES, left(c)); };
     auto place_of = [&](int j) { return (long)__builtin_amdgcn_readlane(place, j); };
     auto weight_of = [&](int j) { return lane_of(weight, j); };
 
@@ -125,15 +132,15 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
     chunk_t keep[NV] = {};
 #pragma unroll
     for (int k = 0; k < NV; ++k)
-        if (c0 + k * STEP < cols) keep[k] = take8(x + (long)(c0 + k * STEP) * ES, cols - c0 - k * STEP);
+        if (c0 + k * STEP < cols) keep[k] = TO_F8 ? take8(x + (long)(c0 + k * STEP) * ES, cols - c0 - k * STEP) : take(x, c0 + k * STEP);
     auto each = [&](auto f) { // of the lane's chunks
 #pragma unroll
         for (int k = 0; k < NV; ++k)
             if (c0 + k * STEP < cols) f(c0 + k * STEP, keep[k]);
-        for (int c = c0 + NV * STEP; c < cols; c += STEP) f(c, take8(x + (long)c * ES, cols - c));
+        for (int c = c0 + NV * STEP; c < cols; c += STEP) f(c, take(x, c));
     };
     auto to_all = [&](int c, const auto &o) {
-        for (unsigned long m = real; m; m &= m - 1) give8(y + (place_of(__builtin_ctzl(m)) * g.cols + c) * OS, o, cols - c);
+        for (unsigned long m = real; m; m &= m - 1) give8(y + (place_of(__builtin_ctzl(m)) * g.cols + begin(c)) * OS, o, left(c));
     };
     if constexpr (TO_I8) {
         __shared__ unsigned parts[THREADS / 64];
@@ -221,29 +228,38 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
             }
         }
     }
-#elif MODE == 1
+#else
+    // the token's choices AT_ONCE at a time, their rows in flight together
+    constexpr int AT_ONCE = 4;
+    auto batches = [&](auto f) { // f(places, numbers, how many)
+        for (unsigned long m = real; m;) {
+            long p[AT_ONCE];
+            int j[AT_ONCE], n = 0;
+#pragma unroll
+            for (int u = 0; u < AT_ONCE; ++u) {
+                j[u] = m ? __builtin_ctzl(m) : 0;
+                p[u] = place_of(j[u]);
+                n += m != 0;
+                m &= m - 1;
+            }
+            f(p, j, n);
+        }
+    };
+#if MODE == 1
     const char *x = g.x + inst * g.x_inst, *r = g.c + at * g.cols * OS;
     char *y = g.y + at * g.cols * OS;
     for (int c = c0; c < cols; c += STEP) {
-        const int n = cols - c;
         float sum[8] = {0, 0, 0, 0, 0, 0, 0, 0};
         if (RESIDUAL) {
-            const results_t o = take_results(r + (long)c * OS, n);
+            const results_t o = take_results(r + (long)begin(c) * OS, left(c));
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] = value_of(o.v[i]);
         }
-        unsigned long m = real;
-        while (m) {
-            constexpr int AT_ONCE = 4; // rows in flight
+        batches([&](const long (&p)[AT_ONCE], const int (&j)[AT_ONCE], int count) {
             chunk_t v[AT_ONCE];
-            int j[AT_ONCE], count = 0;
 #pragma unroll
-            for (int u = 0; u < AT_ONCE; ++u) {
-                j[u] = m ? __builtin_ctzl(m) : j[0]; // behind the last the first once more, not added
-                count += m != 0;
-                m &= m - 1;
-                v[u] = take8(x + place_of(j[u]) * g.x_row + (long)c * ES, n);
-            }
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (u < count) v[u] = take(x + p[u] * g.x_row, c);
 #pragma unroll
             for (int u = 0; u < AT_ONCE; ++u)
                 if (u < count) {
@@ -251,47 +267,55 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
 #pragma unroll
                     for (int i = 0; i < 8; ++i) sum[i] = __builtin_fmaf(w, to_acc(v[u].v[i]), sum[i]);
                 }
-        }
+        });
         results_t o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o.v[i] = round_out(sum[i]);
-        give8(y + (long)c * OS, o, n);
+        if (RESIDUAL && c > cols - 8) { // R may be Y: what the lane before shares with this one is its to write
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (begin(c) + i >= c && i < left(c)) reinterpret_cast<out_t *>(y)[begin(c) + i] = o.v[i];
+        } else {
+            give8(y + (long)begin(c) * OS, o, left(c));
+        }
     }
 #else
     const char *x = g.x + inst * g.x_inst + (live ? token : 0) * g.x_row, *other = g.c + inst * g.c_inst;
     char *y = g.y + (long)inst * g.rows * g.cols * OS;
     __shared__ float parts[THREADS / 64][64];
-    chunk_t keep[NV] = {};
-#pragma unroll
-    for (int k = 0; k < NV; ++k)
-        if (c0 + k * STEP < cols) keep[k] = take8(x + (long)(c0 + k * STEP) * ES, cols - c0 - k * STEP);
     float dots = 0; // of choice j in lane j
-    for (unsigned long m = real; m; m &= m - 1) {
-        const int j = __builtin_ctzl(m);
-        const long p = place_of(j);
-        const float w = weight_of(j);
-        const char *from = other + p * g.c_row;
-        char *to = y + p * g.cols * OS;
-        float dot = 0;
-        auto one = [&](int c, const chunk_t &v, const chunk_t &q) {
-            results_t o;
+    for (int c1 = part * 512; c1 < cols; c1 += STEP) { // all lanes together: their sums are added up
+        const int c = c1 + lane * 8, from = begin(c), n = left(c);
+        const bool there = c < cols;
+        chunk_t v = {};
+        if (wide || there) v = take(x, c);
+        const bool tail = c1 + 512 > cols; // some lanes have columns that are not to be counted: none, or the lane before's
+        batches([&](const long (&p)[AT_ONCE], const int (&j)[AT_ONCE], int count) {
+            chunk_t q[AT_ONCE];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                dot = __builtin_fmaf(to_acc(v.v[i]), to_acc(q.v[i]), dot);
-                o.v[i] = round_out(w * to_acc(v.v[i]));
-            }
-            give8(to + (long)c * OS, o, cols - c);
-        };
-        chunk_t q[NV];
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (u < count && (wide || there)) q[u] = take(other + p[u] * g.c_row, c);
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (c0 + k * STEP < cols) q[k] = take8(from + (long)(c0 + k * STEP) * ES, cols - c0 - k * STEP);
+            for (int u = 0; u < AT_ONCE; ++u)
+                if (u < count) {
+                    const float w = weight_of(j[u]);
+                    if (tail) {
 #pragma unroll
-        for (int k = 0; k < NV; ++k)
-            if (c0 + k * STEP < cols) one(c0 + k * STEP, keep[k], q[k]);
-        for (int c = c0 + NV * STEP; c < cols; c += STEP) one(c, take8(x + (long)c * ES, cols - c), take8(from + (long)c * ES, cols - c));
-        dot = sum_wave(dot);
-        dots = lane == j ? dot : dots;
+                        for (int i = 0; i < 8; ++i)
+                            if (!there || from + i < c) q[u].v[i] = in_t(0);
+                    }
+                    float dot = 0;
+                    results_t o;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        dot = __builtin_fmaf(tail && (!there || from + i < c) ? 0.f : to_acc(v.v[i]), to_acc(q[u].v[i]), dot);
+                        o.v[i] = round_out(w * to_acc(v.v[i]));
+                    }
+                    if (there) give8(y + (p[u] * g.cols + from) * OS, o, n);
+                    dot = sum_wave(dot);
+                    dots += lane == j[u] ? dot : 0.f;
+                }
+        });
     }
     if (WAVES > 1) {
         parts[wave][lane] = dots;
@@ -301,5 +325,6 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
         for (int i = 0; i < WAVES; ++i) dots += parts[group * WAVES + i][lane];
     }
     if (part == 0 && lane < chosen) g.s[at * g.chosen + lane] = dots;
+#endif
 #endif
 }

@@ -45,7 +45,7 @@ __device__ __forceinline__ void wave_lds()
 constexpr int CH = 16 / (int)sizeof(in_t) < VALUES ? 16 / (int)sizeof(in_t) : VALUES;
 __device__ __forceinline__ int expert_of(int i, int l) { return (i / CH * LANES + l) * CH + i % CH; }
 struct __attribute__((packed, aligned(sizeof(in_t)))) logits_t { in_t v[CH]; };
-// The logits of a lane, `none` where there is no expert.
+// The logits of a lane, `none` where there is no expert.  All loads of a chunk are on their way together: none is behind a branch of its own.
 __device__ __forceinline__ void load_logits(const in_t *row, int l, int experts, float none, float (&x)[VALUES])
 {
 #pragma unroll
@@ -57,10 +57,9 @@ __device__ __forceinline__ void load_logits(const in_t *row, int l, int experts,
             for (int i = 0; i < CH; ++i) x[c + i] = to_acc(q.v[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < CH; ++i) {
-                x[c + i] = none;
-                if (e + i < experts) x[c + i] = to_acc(row[e + i]);
-            }
+            for (int i = 0; i < CH; ++i) x[c + i] = to_acc(row[e + i < experts ? e + i : experts - 1]);
+#pragma unroll
+            for (int i = 0; i < CH; ++i) x[c + i] = e + i < experts ? x[c + i] : none;
         }
     }
 }

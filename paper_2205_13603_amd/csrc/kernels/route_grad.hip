@@ -38,8 +38,8 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const route_grad
     const int lane = threadIdx.x % 64, l = lane % LANES, wave = threadIdx.x / 64, inst = blockIdx.y;
     const int token = ((int)blockIdx.x * WAVES + wave) * TOKENS + lane / LANES;
     const bool live = token < g.tokens;
-    const int experts = live ? g.experts : 0;
-    const in_t *row = g.x + inst * g.x_inst + (live ? token : 0) * g.x_row;
+    const int experts = g.experts;
+    const in_t *row = g.x + inst * g.x_inst + (live ? token : g.tokens - 1) * g.x_row;
     const long at = (long)inst * g.tokens + (live ? token : 0);
     float *const mine = parts[wave * TOKENS + lane / LANES];
 
@@ -158,9 +158,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const route_grad
             if constexpr (DENSE) y = x[c + i] * inverse * (y - dot);
             o.v[i] = round_in(y);
         }
-        if (e + CH <= experts) {
+        if (live && e + CH <= experts) {
             *reinterpret_cast<logits_t *>(to + e) = o;
-        } else {
+        } else if (live) {
 #pragma unroll
             for (int i = 0; i < CH; ++i)
                 if (e + i < experts) to[e + i] = o.v[i];

@@ -683,6 +683,7 @@ extern "C" int32_t ms_space_describe(const ms_op *op, uint32_t flags, ms_space *
     if (is_layer(d.kind)) { // no module changes their kernels; the one decision is what a workgroup works on
         out->family = layer_family(d.kind);
         if (is_route(d.kind)) add_cat(out, MS_SLOT_BLOCK, "block", {0, 8, 16, 32, 64});
+        else if (moves_rows(d.kind)) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 3, 4, 5, 6, 8, 10, 12, 14, 16});
         else if (is_routing(d.kind)) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
         else if (d.kind == MS_OP_RMS_NORM) add_cat(out, MS_SLOT_BLOCK, "block", {0, 1, 2, 4, 8, 16});
         else add_cat(out, MS_SLOT_BLOCK, "block", {0, 16016, 16032, 32032, 64032, 64128, 128128, 256256});

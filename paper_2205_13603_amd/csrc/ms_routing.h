@@ -212,6 +212,7 @@ inline void routing_work(const ms_op *op, double *flop, double *bytes)
 
 inline bool routing_block_fits(const ms_op *op, int64_t code)
 {
+    if (moves_rows(op->d.kind)) return code >= 1 && code <= 16;
     if (code < 1 || (code & (code - 1))) return false;
     if (is_route(op->d.kind)) return code >= 8 && code <= 64 && power_of_two(op->K) <= 32 * code; // 32 experts of a lane
     return code <= 16;
@@ -223,17 +224,23 @@ inline int64_t routing_rule(const ms_op *op)
     const int64_t T = op->M;
     if (is_route(op->d.kind)) {
         int64_t lanes = 64;
-        while (lanes > 8 && T * lanes > 64 * 2048 && routing_block_fits(op, lanes / 2)) lanes /= 2;
+        while (lanes > 8 && T * lanes > 64 * (power_of_two(op->K) > 8 * lanes ? 2048 : 1024) && routing_block_fits(op, lanes / 2)) lanes /= 2;
         return lanes;
     }
     if (op->d.kind == MS_OP_EXPERT_ORDER) {
+        // One workgroup up to 4096 choices (256 experts, 2400 choices: 4.9 us, in three runs 6.9; 8192: 8.1 and 6.8); beyond, runs of one choice of a lane until their
+        // counts are many (256 experts, 131072 choices by 1, 2, 4: 7.1, 7.2, 8.5; 1024 experts: 13.4, 11.2, 11.8; 524288 choices, 256 experts: 18.0, 10.0, 9.8).
         int64_t rounds = 1;
-        while (rounds < 16 && T * op->N > 256 * 1024 * rounds) rounds *= 2;
+        const int64_t n = T * op->N;
+        auto runs = [&] { return (n + 1024 * rounds - 1) / (1024 * rounds); };
+        while (rounds < 16 && (n <= 4096 ? runs() > 1 : runs() > 256 || runs() * op->K > 65536)) rounds *= 2;
         return rounds;
     }
-    int64_t waves = 1;
-    while (waves < 16 && waves * 512 < op->N && (T * waves < 2048 || waves * 2048 < op->N)) waves *= 2;
-    return waves;
+    // a chunk for each wavefront, or as many for all of them
+    const int64_t chunks = (op->N + 511) / 512, passes = (chunks + 15) / 16, waves = (chunks + passes - 1) / passes;
+    for (int64_t w : {1, 2, 3, 4, 5, 6, 8, 10, 12, 14})
+        if (w >= waves) return w;
+    return 16;
 }
 
 inline int order_threads(const ms_op *op) { return op->M * op->N <= 64 ? 64 : op->M * op->N <= 256 ? 256 : 1024; }
@@ -251,6 +258,14 @@ inline size_t routing_workspace(const ms_op *op, const ms_variant_params *p) // 
 }
 inline int route_values(const ms_op *op, int64_t lanes) { return (int)std::max<int64_t>(1, power_of_two(op->K) / lanes); }
 inline bool route_grouped(const ms_op *op) { return op->d.kind == MS_OP_ROUTE && op->d.dims[3] > 1; }
+inline int route_chunk(const ms_op *op, int64_t lanes) { return std::min(16 / op->in_size, route_values(op, lanes)); } // neighbouring experts of a lane
+// Experts of a group where its best are found in the registers of lanes: a power of two, whole chunks, up to 16 groups; else 0, by way of LDS.
+inline int64_t route_group_size(const ms_op *op, int64_t lanes)
+{
+    if (!route_grouped(op)) return 0;
+    const int64_t size = op->K / op->d.dims[3];
+    return power_of_two(size) == size && size >= route_chunk(op, lanes) && lanes * route_values(op, lanes) <= 16 * size ? size : 0;
+}
 // one expert that speaks for a group, where there are no groups
 inline int route_best(const ms_op *op) { return route_grouped(op) ? (int)op->d.dims[5] : 1; }
 
@@ -261,13 +276,14 @@ inline void resolve_routing(const ms_op *op, int64_t code, ms_variant_params *p,
     if (is_route(op->d.kind)) {
         const int values = route_values(op, code), room = (int)code * values;
         p->body = MS_BODY_ROUTE;
-        p->waves = route_grouped(op) ? 1 : 4; // groups: by way of LDS
+        const bool in_lds = route_grouped(op) && !route_group_size(op, code);
+        p->waves = in_lds ? 1 : 4;
         p->threads = 64 * p->waves;
         p->block_m = p->threads / (int)code;
         p->block_k = room;
-        p->vec = std::min(16 / op->in_size, values);
+        p->vec = route_chunk(op, code);
         p->acc_per_thread = 2 * values + 2 * (int)power_of_two(op->N);
-        p->lds_bytes = op->d.kind == MS_OP_ROUTE_GRAD ? p->block_m * (room + 4) * 4 : route_grouped(op) ? p->block_m * (room + room / 32 + 4 + MS_MAX_GROUPS + 1) * 8 : 0;
+        p->lds_bytes = op->d.kind == MS_OP_ROUTE_GRAD ? p->block_m * (room + 4) * 4 : in_lds ? p->block_m * (room + room / 32 + 4 + (int)power_of_two(op->d.dims[3]) + 1) * 8 : 0;
         *grid = (op->M + p->block_m - 1) / p->block_m;
     } else if (op->d.kind == MS_OP_EXPERT_ORDER) {
         const int experts = order_experts(op);
@@ -281,7 +297,7 @@ inline void resolve_routing(const ms_op *op, int64_t code, ms_variant_params *p,
         *grid = order_runs(op, code);
     } else {
         p->body = MS_BODY_EXPERT_ROWS;
-        p->waves = std::max(4, (int)code);
+        p->waves = code < 3 ? 4 : (int)code;
         p->threads = p->waves * 64;
         p->block_m = p->waves / (int)code;
         p->block_k = (int)code * 512;
@@ -307,6 +323,8 @@ template <class Def> std::string routing_spec(const ms_op *op, const ms_variant_
         D.push_back(def("BIAS", d.has_bias));
         D.push_back(def("GROUPED", route_grouped(op)));
         D.push_back(def("BEST", route_best(op)));
+        D.push_back(def("GROUP_SIZE", route_group_size(op, p->body_tile)));
+        if (route_grouped(op) && !route_group_size(op, p->body_tile)) D.push_back(def("GROUPS", power_of_two(op->d.dims[3])));
         return "route.hip";
     }
     if (d.kind == MS_OP_EXPERT_ORDER) {

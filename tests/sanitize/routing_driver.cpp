@@ -136,12 +136,12 @@ int main()
     // a workgroup for so many tokens
     g_launches.clear();
     v = build(MS_OP_ROUTE, MS_F32, MS_F32, {100, 256, 8, 8, 4, 2, 3, 0}, 16, 1);
-    CHECK(ms_variant_launch(v, in, out, nullptr, 1, nullptr) == MS_OK && g_launches[0].x == 25 && g_launches[0].threads == 64);
+    CHECK(ms_variant_launch(v, in, out, nullptr, 1, nullptr) == MS_OK && g_launches[0].x == 7 && g_launches[0].threads == 256);
     in[1] = nullptr;
     CHECK(ms_variant_launch(v, in, out, nullptr, 1, nullptr) == MS_ERR_BAD_ARG);
     ms_variant_destroy(v);
-    v = build(MS_OP_ROUTE, MS_F32, MS_F32, {100, 256, 8, 1, 1, 1, 0, 0}, 16);
-    CHECK(ms_variant_launch(v, in, out, nullptr, 1, nullptr) == MS_OK && g_launches[1].x == 7 && g_launches[1].threads == 256);
+    v = build(MS_OP_ROUTE, MS_F32, MS_F32, {100, 240, 8, 8, 4, 2, 3, 0}, 16); // groups of 30: by way of LDS
+    CHECK(ms_variant_launch(v, in, out, nullptr, 1, nullptr) == MS_OK && g_launches[1].x == 25 && g_launches[1].threads == 64);
     ms_variant_destroy(v);
     v = build(MS_OP_JOIN_ROWS, MS_BF16, MS_BF16, {100, 4, 4096, 400, 0}, 8);
     in[1] = a;

@@ -785,7 +785,7 @@ def test_a_layer_of_experts_in_8_bit_integers():
 
 def test_captured_layer_follows_its_inputs():
     """Forward and backward in one graph, replayed with other logits and rows and the program's own eager run in between; the order needs its workspace."""
-    T, E, K, F, N = 1300, 16, 2, 64, 72
+    T, E, K, F, N = 2200, 16, 2, 64, 72
     layer = Layer(T, E, K, F, N, "bf16")
     if layer.ops["route"] is None:
         return
@@ -803,7 +803,7 @@ def test_captured_layer_follows_its_inputs():
     with torch.cuda.graph(graph):
         step()
     names = [n for n in o if n != "ws"]
-    for masked in (0, 1299, 1300, 50):
+    for masked in (0, 2199, 2200, 50):
         for k, t in layer.inputs(g, masked).items():
             d[k].copy_(t)
         got = []

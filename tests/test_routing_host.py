@@ -234,8 +234,8 @@ def test_rules():
     lanes = [block(B.route_op(T, 256, 8)) for T in (1, 100, 3000, 6000, 16384, 100000)]
     assert lanes[0] == 64 and lanes[-1] == 8 and lanes == sorted(lanes, reverse=True)
     assert block(B.route_op(100000, 1024, 8)) == 32 and block(B.route_op(100000, 300, 8)) == 16
-    assert block(B.join_rows_op(1, 8, 8192, 8)) == 16 and block(B.join_rows_op(10000, 8, 512, 80000)) == 1 and block(B.join_rows_op(1, 8, 512, 8)) == 1
-    assert [block(B.expert_order_op(8, T, 8)) for T in (1, 16384)] == [1, 1] and block(B.expert_order_op(8, 1 << 20, 8)) > 1
+    assert [block(B.join_rows_op(9, 8, N, 72)) for N in (8, 512, 513, 2050, 8192, 8193, 20000)] == [1, 1, 2, 5, 16, 10, 14]
+    assert [block(B.expert_order_op(8, T, 8)) for T in (1, 500, 16384, 1 << 20)] == [1, 4, 1, 16]
 
 
 def test_sampled_composed_and_searched():
