@@ -160,7 +160,7 @@ typedef enum ms_dtype { MS_F32 = 0, MS_F16 = 1, MS_BF16 = 2, MS_I8 = 3, MS_I32 =
  *                 Scores s = softmax(X[t]), or sigmoid(X[t]) with MS_ROUTE_SIGMOID.  Choice c = s + bias (has_bias 1) or s.  With groups > 1 (of E / groups neighbouring
  *                 experts) the `kept` groups with the largest sums of their `best` largest c take part, a group with fewer experts to choose by those it has.
  *                 ids[t] are the K experts with the largest c, in that order, the lower index first among equals; W their scores s, with
- *                 MS_ROUTE_RENORMALISE over their sum (0 / 0 is NaN), times the scale.  c is computed in 64 bits and told apart down to 2^-41 of its size, so
+ *                 MS_ROUTE_RENORMALISE over their sum (0 / 0 is NaN), times the scale.  c is computed in 64 bits and told apart down to 2^-41 of the larger of s and |bias|, so
  *                 that a choice does not hang on how fp32 rounds; without a bias, and without groups or with best = 1, the logits themselves are compared.
  *                 Experts whose logit is -infinity or NaN, or whose c is, cannot be chosen; where fewer than K can, the remaining ids are -1 and their weights 0.
  *                 A NaN among a token's logits (softmax: or +infinity) makes all its weights NaN.

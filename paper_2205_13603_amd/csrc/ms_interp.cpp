@@ -862,7 +862,7 @@ int32_t resolve_layer(const ms_op *op, const ms_space *space, const ms_trace *tr
         p->lds_bytes = (int32_t)t.lds;
         grid = ragged_tiles(op, t);
     }
-    if (grid > 0x7fffffff || (p->family == MS_FAM_RAGGED && grid * p->threads > 0xffffffffll)) return reject("grid of %" PRId64 " workgroups overflows", grid);
+    if (grid > 0x7fffffff || (p->family != MS_FAM_RMS_NORM && grid * p->threads > 0xffffffffll)) return reject("grid of %" PRId64 " workgroups overflows", grid);
     p->grid[0] = (int32_t)grid;
     p->body_tile = (int32_t)code;
     if (p->threads > g_limits.max_threads || p->waves > g_limits.max_waves) return reject("%d threads per workgroup, the limit is %d", p->threads, g_limits.max_threads);

@@ -625,6 +625,60 @@ def test_rows_strides_and_instances():
                     assert bool(((dc[r, p].double() - want).abs() <= want.abs() * 2.0 ** -8 * 1.01).all())
 
 
+@pytest.mark.parametrize("N", [1, 3, 7, 8, 9, 511, 513])
+def test_rows_of_few_columns_and_ends(N):
+    """Rows shorter than a lane's eight columns, and just beside; rows in place of the residual, whose ends two lanes share."""
+    T, K, P = 13, 3, 39
+    for kind in ("bf16", "f32"):
+        ops = [variant(o) for o in (B.spread_rows_op(T, K, N, P, kind), B.spread_rows_op(T, K, N, P, kind, "i8"), B.spread_rows_op(T, K, N, P, kind, "f8"), B.join_rows_op(T, K, N, P, kind, residual=True),
+                                    B.join_rows_op(T, K, N, P, kind), B.join_grad_op(T, K, N, P, kind))]
+        if ops[0] is None:
+            continue
+        g = rng(N)
+        place = places_of(g, T, K, P)
+        x, c, w, r = normal(g, T, N).to(TYPES[kind]), normal(g, P, N).to(TYPES[kind]), normal(g, T, K), normal(g, T, N).to(TYPES[kind])
+        blocks = -(-N // 128)
+        (a, _) = call(ops[0], [dev(x), dev(place), None], [((P, N), TYPES[kind]), None])
+        check_spread(a, None, x, place, None, kind, 0)
+        a, s = call(ops[1], [dev(x), dev(place), None], [((P, N), torch.int8), ((P, 1), torch.float32)])
+        check_spread(a, s, x, place, None, "i8", 1)
+        a, s = call(ops[2], [dev(x), dev(place), None], [((P, N), TYPES["f8"]), ((P, blocks), torch.float32)])
+        check_spread(a, s, x, place, None, "f8", blocks)
+        for v, res in ((ops[3], r), (ops[4], None)):
+            (y,) = call(v, [dev(c), dev(place), dev(w), dev(res)], [((T, N), TYPES[kind])])
+            want, mag = join_definition(c, place, w, res)
+            assert bool(((y.double() - want).abs() <= mag * (K + 1) * 2.0 ** -24 + want.abs() * (HALF_STEP[kind] if kind != "f32" else 0) * 1.01 + 1e-37).all())
+            if res is not None:
+                d, dp, dw, dr = dev(c), dev(place), dev(w), dev(res)
+                v.launch([d.data_ptr(), dp.data_ptr(), dw.data_ptr(), dr.data_ptr()], dr.data_ptr(), stream=devmem.current_stream())
+                torch.cuda.synchronize()
+                assert torch.equal(dr.cpu(), y)
+        dc, dw = call(ops[5], [dev(x), dev(place), dev(w), dev(c)], [((P, N), TYPES[kind]), ((T, K), torch.float32)])
+        for t in range(T):
+            for j in range(K):
+                p = int(place[t, j])
+                if 0 <= p < P:
+                    products = x[t].double() * c[p].double()
+                    assert abs(float(dw[t, j]) - float(products.sum())) <= float(products.abs().sum()) * (N / 64 + 32) * 2.0 ** -24
+                    want = x[t].double() * float(w[t, j])
+                    assert bool(((dc[p].double() - want).abs() <= want.abs() * HALF_STEP[kind] * 1.01).all())
+                else:
+                    assert float(dw[t, j]) == 0
+
+
+def test_infinities_at_the_shared_end_of_a_row():
+    """What two lanes hold of a row's end counts once: an infinity stays one."""
+    T, N = 2, 1003
+    v = variant(B.join_grad_op(T, 1, N, T, "f32"))
+    if v is None:
+        return
+    dy, c, w = torch.ones(T, N), torch.ones(T, N), torch.ones(T, 1)
+    c[0, N - 6], c[1, N - 1] = INF, -INF
+    place = torch.arange(T).int().view(T, 1)
+    dc, dw = call(v, [dev(dy), dev(place), dev(w), dev(c)], [((T, N), torch.float32), ((T, 1), torch.float32)])
+    assert dw.reshape(-1).tolist() == [INF, -INF] and bool((dc == 1).all())
+
+
 def test_rows_beyond_4_gib():
     """Places behind the first 4 GiB of rows, of tokens behind theirs."""
     T, K, N = 330000, 1, 8192

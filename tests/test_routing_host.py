@@ -171,6 +171,8 @@ def test_refused_operators():
     refused(no, B.Op, B.OP_JOIN_GRAD, "f16", "f32", [4, 2, 8, 8])
     refused(bad, B.join_grad_op, 4, 2, 8, 8, b_strides=[0, 7, 1])
     refused(bad, B.join_grad_op, 4, 2, 8, 8, a_strides=[1, 8, 1])
+    for op in (B.route_op(1 << 30, 8, 2), B.route_grad_op(1 << 30, 8, 2), B.join_rows_op(1 << 27, 1, 8, 8), B.spread_rows_op(1 << 27, 1, 8, 8)):  # more threads than a grid has
+        refused(B.MS_ERR_INVALID_TRACE, B.trace_validate, op, op.space(), B.default_trace(op.space()))
 
 
 def test_refused_launches():
