@@ -9,6 +9,10 @@
 // WAVES wavefronts share a token, 8 neighbouring columns of a lane in each chunk of 512 columns; OUT keeps up to NV chunks in registers and reads what
 // lies beyond again.  A token's places and weights lie in the lanes of each of its wavefronts, from where scalar registers take them: a row's
 // address is computed once, by the scalar unit.
+//
+// What bounds it is memory: bf16, 4096 x 2048 to 8 choices into 8-bit integers 14.8 us (5.7 TB/s), as they are 26.2 (5.8); back 28.4 (5.3, rows of 4 KiB read in any
+// order); gradients 57 (5.0, as much written as read; 3000 x 2050 to 6 choices, whose rows are no whole 16 bytes, 30 to 36 by what the card's last level cache
+// holds).  Results stay out of the L2s: kept there 4096 x 2048 to 8 choices takes 32 us instead of 26, back 32 instead of 28.  Few tokens: the launch.
 #include "common.h"
 #include "rows.h"
 
@@ -24,7 +28,7 @@ struct rows_args {
 };
 
 constexpr int NV = 4, THREADS = WAVES < 3 ? 256 : WAVES * 64, GROUPS = THREADS / 64 / WAVES, STEP = WAVES * 512;
-constexpr int OUT = 0, BACK = 1, GRAD = 2, ES = sizeof(in_t), OS = sizeof(out_t);
+constexpr int ES = sizeof(in_t), OS = sizeof(out_t);
 constexpr bool BYTES = ES == 1, TO_I8 = OUT_DT == DT_I8 && !BYTES, TO_F8 = OUT_DT == DT_F8E4M3 && !BYTES;
 
 struct bytes_t { char v[8]; };
@@ -119,14 +123,14 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
     if (lane < chosen) {
         place = g.place ? g.place[at * g.chosen + lane] : token;
         if (place >= g.rows) place = -1;
-        if (MODE != OUT && g.w) weight = g.w[at * g.chosen + lane];
+        if (g.w) weight = g.w[at * g.chosen + lane];
     }
     const unsigned long real = __ballot(place >= 0);
     auto take = [&](const char *row, int c) { return take8(row + (long)begin(c) * ES, left(c)); };
     auto place_of = [&](int j) { return (long)__builtin_amdgcn_readlane(place, j); };
     auto weight_of = [&](int j) { return lane_of(weight, j); };
 
-#if MODE == 0
+#if MODE == 0 // OUT
     const char *x = g.x + inst * g.x_inst + (live ? token : 0) * g.x_row;
     char *y = g.y + (long)inst * g.rows * g.cols * OS;
     chunk_t keep[NV] = {};
@@ -245,7 +249,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const rows_args 
             f(p, j, n);
         }
     };
-#if MODE == 1
+#if MODE == 1 // BACK
     const char *x = g.x + inst * g.x_inst, *r = g.c + at * g.cols * OS;
     char *y = g.y + at * g.cols * OS;
     for (int c = c0; c < cols; c += STEP) {

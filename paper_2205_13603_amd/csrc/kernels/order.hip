@@ -5,6 +5,8 @@
 // atomic operation decides an order, so that the result is the same every time.
 //
 // More choices than one workgroup takes: a first kernel counts each run's experts (counts), and each workgroup adds up what lies ahead of its own.
+//
+// What bounds it is latency: 16 choices 4.5 us, the launch; 131072 choices of 256 experts 7.2, of which the second launch is 2; 524288 10.0.
 #include "common.h"
 
 struct order_args {
@@ -41,6 +43,7 @@ __device__ __forceinline__ int id_at(const order_args &g, const int *ids, int n)
     return id >= 0 && id < g.experts ? id : -1;
 }
 
+#if MANY
 extern "C" __global__ void __launch_bounds__(THREADS) ms_count(const order_args g)
 {
     __shared__ int count[EXPERTS];
@@ -57,6 +60,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_count(const order_args 
     int *to = g.counts + ((long)inst * g.runs + blockIdx.x) * g.experts;
     for (int e = tid; e < g.experts; e += THREADS) to[e] = count[e];
 }
+#endif
 
 extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const order_args g)
 {

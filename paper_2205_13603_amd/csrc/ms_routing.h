@@ -223,20 +223,34 @@ inline int64_t routing_rule(const ms_op *op)
 {
     const int64_t T = op->M;
     if (is_route(op->d.kind)) {
+        // Fewer lanes have less to exchange, more of them finish sooner: a wavefront for each SIMD, four where a lane would get 32 experts.  256 experts by groups,
+        // choices of 8, by lanes: 1 token 64: 4.5 us, 8: 7.3; 2048 tokens 64: 4.8, 32: 4.4, 8: 7.7; 8192 32: 8.0, 16: 6.9, 8: 7.4; 16384 32: 14.2, 16: 12.3, 8: 13.0.
+        // 512 experts, choices of 16, 16384 tokens: 32: 24.1, 16: 21.3.  128 experts, 16384 tokens: 16: 5.1, 8: 4.4.
         int64_t lanes = 64;
-        while (lanes > 8 && T * lanes > 64 * (power_of_two(op->K) > 8 * lanes ? 2048 : 1024) && routing_block_fits(op, lanes / 2)) lanes /= 2;
+        while (lanes > 8 && T * lanes > 64 * (power_of_two(op->K) > 8 * lanes ? 4096 : 1024) && routing_block_fits(op, lanes / 2)) lanes /= 2;
         return lanes;
     }
     if (op->d.kind == MS_OP_EXPERT_ORDER) {
-        // One workgroup up to 4096 choices (256 experts, 2400 choices: 4.9 us, in three runs 6.9; 8192: 8.1 and 6.8); beyond, runs of one choice of a lane until their
-        // counts are many (256 experts, 131072 choices by 1, 2, 4: 7.1, 7.2, 8.5; 1024 experts: 13.4, 11.2, 11.8; 524288 choices, 256 experts: 18.0, 10.0, 9.8).
-        int64_t rounds = 1;
+        // One workgroup up to 4096 choices (256 experts, 2400 choices: 4.9 us, in three runs 6.9; 8192: 8.1 and 6.8).  Beyond, the least of what a workgroup takes for
+        // its choices, 0.75 us for each of a lane, and for the counts of all runs, 120 bytes a nanosecond, in as many turns as 256 compute units need (256 experts,
+        // 131072 choices by 1, 2, 4: 7.1, 7.2, 8.5; 1024 experts: 13.4, 11.2, 11.8; 524288 choices, 256 experts: 18.0, 10.0, 9.8).
         const int64_t n = T * op->N;
-        auto runs = [&] { return (n + 1024 * rounds - 1) / (1024 * rounds); };
-        while (rounds < 16 && (n <= 4096 ? runs() > 1 : runs() > 256 || runs() * op->K > 65536)) rounds *= 2;
+        int64_t rounds = 1;
+        if (n <= 4096) {
+            while (1024 * rounds < n) rounds *= 2;
+            return rounds;
+        }
+        double least = 0;
+        for (int64_t r = 1; r <= 16; r *= 2) {
+            const int64_t runs = (n + 1024 * r - 1) / (1024 * r);
+            const double time = (double)((runs + 255) / 256) * (0.75 * (double)r + (double)(runs * op->K) / 30000);
+            if (r == 1 || time < least) least = time, rounds = r;
+        }
         return rounds;
     }
-    // a chunk for each wavefront, or as many for all of them
+    // A chunk of 512 columns for each wavefront, or as many for all of them.  bf16, by wavefronts to a token: 4096 x 2048 into 8-bit integers for 8 choices 4: 14.8 us, 1:
+    // 16.6, 16: 22; 8 rows of 4096 x 2048 back 4: 28.4, 1: 35.8; 7 tokens of 4096 columns back 8: 4.5, 1: 16; gradients of 512 x 8192 for 4 choices 16: 12.6, 4: 14.9.
+    // fp32, 15276 x 4827 into 8-bit integers for 5 choices 10: 135, 16: 144, 4: 171.
     const int64_t chunks = (op->N + 511) / 512, passes = (chunks + 15) / 16, waves = (chunks + passes - 1) / passes;
     for (int64_t w : {1, 2, 3, 4, 5, 6, 8, 10, 12, 14})
         if (w >= waves) return w;

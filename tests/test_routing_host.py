@@ -233,11 +233,10 @@ def test_rules():
     def block(op):
         return B.trace_validate(op, op.space(), B.default_trace(op.space())).body_tile
 
-    lanes = [block(B.route_op(T, 256, 8)) for T in (1, 100, 3000, 6000, 16384, 100000)]
-    assert lanes[0] == 64 and lanes[-1] == 8 and lanes == sorted(lanes, reverse=True)
-    assert block(B.route_op(100000, 1024, 8)) == 32 and block(B.route_op(100000, 300, 8)) == 16
+    assert [block(B.route_op(T, 256, 8)) for T in (1, 1024, 2048, 4096, 16384, 100000)] == [64, 64, 32, 16, 16, 8]
+    assert block(B.route_op(100000, 1024, 8)) == 32 and block(B.route_op(100000, 300, 8)) == 16 and block(B.route_op(16384, 60, 6)) == 8
     assert [block(B.join_rows_op(9, 8, N, 72)) for N in (8, 512, 513, 2050, 8192, 8193, 20000)] == [1, 1, 2, 5, 16, 10, 14]
-    assert [block(B.expert_order_op(8, T, 8)) for T in (1, 500, 16384, 1 << 20)] == [1, 4, 1, 16]
+    assert [block(B.expert_order_op(8, T, 8)) for T in (1, 500, 16384, 1 << 20)] == [1, 4, 1, 16] and [block(B.expert_order_op(E, 16384, 8)) for E in (64, 256, 1024)] == [1, 1, 2]
 
 
 def test_sampled_composed_and_searched():
