@@ -16,6 +16,8 @@
 // uncovered, 9 us of stores and first reads for each round of tiles.  8192^3 in 8 bits 450 to 490 us by card and by what ran before (2.2 to 2.4
 // PFLOP/s; loads alone 338, products alone 215 at this clock); bf16, 8 experts, 8192 x 4096 x 4096 230 to 246 (1.1 to 1.2); 8 bits, 32 experts, 16384 x
 // 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 154 to 181 by the experts' rows (0.8 to 0.9, and 2.0 to 2.4 TB/s).
+// 8-bit integers, whose scales meet the sums once, at the end: 8192^3 413 to 422 (2.6 Pop/s, the matrix cores busy two thirds of their cycles), 32
+// experts, 16384 x 2048 x 4096 152 to 155 (1.8).
 //
 // 8-bit floats: the products of a block of 128 k values are one instruction, whose four results per lane are added to the sums
 // with their scales, SA of the lane's row times SB of the wavefront's columns, while the matrix core works on the next.  Scales are
