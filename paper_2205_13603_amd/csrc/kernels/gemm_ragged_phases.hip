@@ -29,10 +29,10 @@
 
 constexpr int BM = 256, BN = 256, WJ = 4, NW = 8, THREADS = NW * 64, TM = 8, TN = 4, BK = 128 / ES;
 constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-constexpr bool SCALED = IN_DT == DT_F8E4M3;
+constexpr bool SCALED = IN_DT == DT_F8E4M3, LINE_SCALED = IN_DT == DT_I8; // scales of blocks of k; of rows and columns
 constexpr int KB = SCALE_RUN, LS = KB * BM / 64 / NW; // k blocks whose scales are in LDS at a time, twice; loads of a wavefront for them
-constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, SB_BYTES = SCALED ? 256 : 0, OS = sizeof(out_t);
-constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, OUT_AT = SB_AT + 2 * SB_BYTES, TABLE_AT = OUT_AT + (OS == 2 ? NW * 1024 : 0);
+constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, LINE_BYTES = LINE_SCALED ? (BM + BN) * 4 : 0, SB_BYTES = SCALED ? 256 : 0, OS = sizeof(out_t);
+constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LINES_AT = SB_AT + 2 * SB_BYTES, OUT_AT = LINES_AT + 3 * LINE_BYTES, TABLE_AT = OUT_AT + (OS == 2 ? NW * 1024 : 0);
 constexpr int LDS_BYTES = TABLE_AT + (WGRAD ? 2048 : GROUPED ? 4096 + 2048 : 0);
 typedef ragged_tile<128, 128, 2, 2, 2> quarter;
 static_assert(quarter::LDS_BYTES <= TABLE_AT, "quarters lie where whole tiles did");
@@ -130,6 +130,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     tile_t lt;
     unsigned lf = blockIdx.x;
     int lk = 0, lsteps = 0, wr = 0, lchunk = 0; // lchunk: which of the two places its run of scales goes to
+    int llines = 0; // which of the three places its tile's scales of rows and columns go to: the cursor may be two tiles ahead of the products
     bool more = true;                           // false: past the last tile, the last step is requested again (never read)
     const char *la, *lb;                        // first row of the step's operands
     unsigned va[4], vb[4]; // of A's parts and B's halves two loads each, from la and lb
@@ -216,6 +217,13 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             for (int l = 0; l < LS; ++l) gather_lds4(buffer_at(lsa + (start + k0 + l) * 4), (unsigned)(start + k0 + l) < (unsigned)blocks ? vsa : OUTSIDE, at + l * BM * 4);
             if (wave == 0) gather_lds4(buffer_at(lsb + start * 4), (unsigned)(start + lane % KB) < (unsigned)blocks ? vsb : OUTSIDE, lds0 + SB_AT + lchunk * SB_BYTES);
         }
+#elif IN_DT == DT_I8
+        if (!inner && lk == first) { // 64 rows of four wavefronts, 64 columns of the others, ahead of the tile's first step
+            const bool of_rows = wave < 4;
+            const char *const from = scalar(of_rows ? (const char *)g.sa + inst * g.sa_inst + (long)lt.row * 4 : (const char *)g.sb + inst * g.sb_inst + ((long)lt.expert * g.cols + lt.col) * 4);
+            const int n = wave % 4 * 64 + lane;
+            gather_lds4(buffer_at(from), n < (of_rows ? lt.rows : g.cols - lt.col) ? (unsigned)n * 4 : OUTSIDE, lds0 + LINES_AT + llines * LINE_BYTES + wave * 256);
+        }
 #endif
     };
     auto next_step = [&]() { // inside the tile
@@ -234,7 +242,10 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         if (more) {
             lf += gridDim.x;
             more = place();
-            if (more) lchunk ^= 1;
+            if (more) {
+                lchunk ^= 1;
+                llines = llines == 2 ? 0 : llines + 1;
+            }
         }
     };
     const tile_t none = {0, 0, 0, 0, 0, 0};
@@ -328,18 +339,17 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #pragma unroll
             for (int j = 0; j < TN; ++j) acc[i][j] = sum4_t{0, 0, 0, 0};
     };
-    auto store = [&](const tile_t &t) {
+    auto store = [&](const tile_t &t, int place) {
         const int lane = opaque(tid % 64), lrow = lane % 16, lgrp = lane / 16;
         char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
         const int cols = g.cols - t.col < BN ? g.cols - t.col : BN;
-        const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + t.row;
-        const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)t.expert * g.cols + t.col;
+        const float *const lines = reinterpret_cast<const float *>(lds + LINES_AT + place * LINE_BYTES);
         f4_t sj[TN];
         float si[TM];
 #pragma unroll
-        for (int j = 0; j < TN; ++j) sj[j] = col_scales(of_cols, wj * 64 + j * 16 + lgrp * 4, cols);
+        for (int j = 0; j < TN; ++j) sj[j] = LINE_SCALED ? *reinterpret_cast<const f4_t *>(lines + BM + wj * 64 + j * 16 + lgrp * 4) : f4_t{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
-        for (int i = 0; i < TM; ++i) si[i] = row_scale(of_rows, wi * 128 + i * 16 + lrow, t.rows);
+        for (int i = 0; i < TM; ++i) si[i] = LINE_SCALED ? lines[wi * 128 + i * 16 + lrow] : 1.f;
         if constexpr (OS == 4) {
 #pragma unroll
             for (int i = 0; i < TM; ++i) {
@@ -400,7 +410,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         zero();
         tile_t t;
         for (unsigned f = blockIdx.x; f < turns; f += gridDim.x)
-            if (tile_of(f, t) && t.depth <= 0) store(t);
+            if (tile_of(f, t) && t.depth <= 0) store(t, 0);
     };
     if (!more) {
         empty_tiles();
@@ -418,7 +428,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
     DL_WAIT_VM(8); // A0 and B of the first step
     barrier();
     if (late) barrier();
-    int rd = 0, cchunk = 0;
+    int rd = 0, cchunk = 0, clines = 0;
     zero();
     for (;;) {
         const int steps = first + (ct.depth + BK - 1) / BK;
@@ -455,7 +465,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         while (reaches && more && lk + 2 < lsteps) step(next_step, true); // requests of steps lk and lk + 1, neither the tile's last
 #pragma unroll 1
         while (k < steps) step(advance, false);
-        store(ct);
+        store(ct, clines);
         zero();
         // the next tile of the products: the one that the cursor found
         bool any = false;
@@ -466,6 +476,7 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
             }
         if (!any) break;
         cchunk ^= 1;
+        clines = clines == 2 ? 0 : clines + 1;
     }
     if (!late) barrier(); // the other group's last phase
     DL_WAIT_VM(0);        // loads past the end land before the workgroup's LDS is released

@@ -224,6 +224,17 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
                     for (int j = 0; j < TN; ++j) acc[i][j] = mfma(fb[q][j], fa[q][i], acc[i][j]);
 #endif
         };
+        constexpr int OS = sizeof(out_t), HALF = TM / GROUPS; // row tiles that this wavefront stores
+        const int row0 = (wi * TM + group * HALF) * 16;
+        // scales of the results' rows and columns (8-bit integers), on their way from here: behind the products they would be waited for
+        const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + t.row;
+        const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)t.expert * g.cols + t.col;
+        f4_t sj[TN];
+        float si[HALF];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sj[j] = col_scales(of_cols, (wj * TN + j) * 16 + lgrp * 4, cols);
+#pragma unroll
+        for (int i = 0; i < HALF; ++i) si[i] = row_scale(of_rows, row0 + i * 16 + lrow, t.rows);
 #if IN_DT == DT_F8E4M3
         if (steps) load_scales(0);
 #endif
@@ -297,17 +308,7 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
         }
 
         // ---- results
-        constexpr int OS = sizeof(out_t), HALF = TM / GROUPS; // row tiles that this wavefront stores
-        const int row0 = (wi * TM + group * HALF) * 16;
         char *c = g.c + inst * g.c_inst + (WGRAD ? (long)t.expert * g.rows * g.cols * OS : 0);
-        const float *const of_rows = (const float *)((const char *)g.sa + inst * g.sa_inst) + t.row;
-        const float *const of_cols = (const float *)((const char *)g.sb + inst * g.sb_inst) + (long)t.expert * g.cols + t.col;
-        f4_t sj[TN];
-        float si[HALF];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) sj[j] = col_scales(of_cols, (wj * TN + j) * 16 + lgrp * 4, cols);
-#pragma unroll
-        for (int i = 0; i < HALF; ++i) si[i] = row_scale(of_rows, row0 + i * 16 + lrow, t.rows);
         if constexpr (OS == 4) {
 #pragma unroll
             for (int i = 0; i < HALF; ++i) {

@@ -140,6 +140,20 @@ def test_tiles_of_which_several_lie_on_a_compute_unit(code):
             check_grouped(v, counts, 1, 2, 4600, K, "bf16")
 
 
+@pytest.mark.parametrize("K", [16, 128, 144, 400])
+@pytest.mark.parametrize("code", [128128, 256256])
+def test_turns_of_few_steps(code, K):
+    """Several tiles for each workgroup, of one step of 128 bytes to four: scales come in ahead of tiles whose products are still to be made."""
+    M, N = 6001, 8200
+    v = variant(B.scaled_gemm_op(M, N, K, "bf16", in_dtype="i8"), code)
+    if v is None:
+        return
+    g = rng(K)
+    a, b, sa, sb = ints(g, M, K), ints(g, N, K), scales(g, M), scales(g, N)
+    (c,) = launch_twice(v, [dev(x) for x in (a, b, sa, sb)], [((M, N), torch.bfloat16)])
+    close(c, a.double() @ b.double().t() * sa.double()[:, None] * sb.double(), "bf16")
+
+
 def test_many_experts():
     E = B.MAX_EXPERTS
     counts = [(e * 7) % 3 for e in range(E)]
