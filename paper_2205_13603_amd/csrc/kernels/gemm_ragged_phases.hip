@@ -16,8 +16,8 @@
 // uncovered, 9 us of stores and first reads for each round of tiles.  8192^3 in 8 bits 450 to 490 us by card and by what ran before (2.2 to 2.4
 // PFLOP/s; loads alone 338, products alone 215 at this clock); bf16, 8 experts, 8192 x 4096 x 4096 230 to 246 (1.1 to 1.2); 8 bits, 32 experts, 16384 x
 // 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 154 to 181 by the experts' rows (0.8 to 0.9, and 2.0 to 2.4 TB/s).
-// 8-bit integers, whose scales meet the sums once, at the end: 8192^3 413 to 422 (2.6 Pop/s, the matrix cores busy two thirds of their cycles), 32
-// experts, 16384 x 2048 x 4096 152 to 155 (1.8).
+// 8-bit integers: 8192^3 402 to 410 (2.7 Pop/s, the matrix cores busy two thirds of their cycles), 32 experts, 16384 x 2048 x 4096 145 to 148 (1.9).
+// Their scales meet the sums once, at the end; they come in by way of LDS with a tile's first step (read there instead, each tile waited 4 us for them).
 //
 // 8-bit floats: the products of a block of 128 k values are one instruction, whose four results per lane are added to the sums
 // with their scales, SA of the lane's row times SB of the wavefront's columns, while the matrix core works on the next.  Scales are
@@ -32,7 +32,7 @@ constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
 constexpr bool SCALED = IN_DT == DT_F8E4M3, LINE_SCALED = IN_DT == DT_I8; // scales of blocks of k; of rows and columns
 constexpr int KB = SCALE_RUN, LS = KB * BM / 64 / NW; // k blocks whose scales are in LDS at a time, twice; loads of a wavefront for them
 constexpr int SC_BYTES = SCALED ? KB * BM * 4 : 0, LINE_BYTES = LINE_SCALED ? (BM + BN) * 4 : 0, SB_BYTES = SCALED ? 256 : 0, OS = sizeof(out_t);
-constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LINES_AT = SB_AT + 2 * SB_BYTES, OUT_AT = LINES_AT + 3 * LINE_BYTES, TABLE_AT = OUT_AT + (OS == 2 ? NW * 1024 : 0);
+constexpr int SC_AT = 2 * STAGE, SB_AT = SC_AT + 2 * SC_BYTES, LINES_AT = SB_AT + 2 * SB_BYTES, TABLE_AT = LINES_AT + 3 * LINE_BYTES;
 constexpr int LDS_BYTES = TABLE_AT + (WGRAD ? 2048 : GROUPED ? 4096 + 2048 : 0);
 typedef ragged_tile<128, 128, 2, 2, 2> quarter;
 static_assert(quarter::LDS_BYTES <= TABLE_AT, "quarters lie where whole tiles did");
@@ -350,52 +350,63 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
         for (int j = 0; j < TN; ++j) sj[j] = LINE_SCALED ? *reinterpret_cast<const f4_t *>(lines + BM + wj * 64 + j * 16 + lgrp * 4) : f4_t{1.f, 1.f, 1.f, 1.f};
 #pragma unroll
         for (int i = 0; i < TM; ++i) si[i] = LINE_SCALED ? lines[wi * 128 + i * 16 + lrow] : 1.f;
-        if constexpr (OS == 4) {
+#if OUT_DT == DT_F32
 #pragma unroll
-            for (int i = 0; i < TM; ++i) {
-                const int r = wi * 128 + i * 16 + lrow;
-                if (r < t.rows) {
+        for (int i = 0; i < TM; ++i) {
+            const int r = wi * 128 + i * 16 + lrow;
+            if (r < t.rows) {
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        const int col = wj * 64 + j * 16 + lgrp * 4;
-                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
+                for (int j = 0; j < TN; ++j) {
+                    const int col = wj * 64 + j * 16 + lgrp * 4;
+                    if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
+                }
+            }
+        }
+#else
+        // A row's 64 columns leave as one line, put together between lanes (by way of LDS: 8-bit integers, 32 experts 148 us instead of 145).  Neighbouring column tiles swap their quads with neighbouring quads of
+        // lanes, so that a lane has eight columns of a row; then the upper eight rows' left halves with the lower ones' right halves.
+        typedef unsigned u2_t __attribute__((ext_vector_type(2)));
+        struct oct_t { unsigned w[4]; };
+        const int col = wj * 64 + lrow / 8 * 32 + lgrp % 2 * 16 + lgrp / 2 * 8;
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+            unsigned of[2][4];
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                u2_t w[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    struct { out_t v[4]; } o;
+                    const f4_t x = results(acc[i][p * 2 + e], si[i], sj[p * 2 + e]);
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) o.v[v] = round_out(x[v]);
+                    w[e] = __builtin_bit_cast(u2_t, o);
+                }
+                const u2_t lo = __builtin_amdgcn_permlane16_swap(w[0][0], w[1][0], false, false), hi = __builtin_amdgcn_permlane16_swap(w[0][1], w[1][1], false, false);
+                of[p][0] = lo[0], of[p][1] = hi[0], of[p][2] = lo[1], of[p][3] = hi[1];
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                oct_t o;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+                    o.w[w] = h ? __builtin_amdgcn_update_dpp(of[1][w], of[0][w], 0x128, 0xf, 0x3, false)  // the other half is that of the lane eight on
+                               : __builtin_amdgcn_update_dpp(of[0][w], of[1][w], 0x128, 0xf, 0xc, false);
+                const int row = wi * 128 + i * 16 + h * 8 + lrow % 8;
+                if (row < t.rows && col < cols) {
+                    char *dst = c + ((long)(t.row + row) * g.cols + t.col + col) * OS;
+                    if (col + 8 <= cols) {
+                        stream_out(dst, o);
+                    } else {
+                        struct { out_t v[8]; } each = __builtin_bit_cast(decltype(each), o);
+#pragma unroll
+                        for (int v = 0; v < 8; ++v)
+                            if (col + v < cols) reinterpret_cast<out_t *>(dst)[v] = each.v[v];
                     }
                 }
             }
-        } else {
-            // 8 rows at a time by way of LDS, so that a row's 64 columns leave as one line
-            char *const mine = lds + OUT_AT + wave * 1024;
-            struct quad_t { out_t v[4]; };
-#pragma unroll
-            for (int i = 0; i < TM; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    if (lrow / 8 == h) {
-#pragma unroll
-                        for (int j = 0; j < TN; ++j) {
-                            quad_t o;
-                            const f4_t x = results(acc[i][j], si[i], sj[j]);
-#pragma unroll
-                            for (int v = 0; v < 4; ++v) o.v[v] = round_out(x[v]);
-                            *reinterpret_cast<quad_t *>(mine + lrow % 8 * 128 + ((j * 2 + lgrp / 2) ^ lrow % 8) * 16 + lgrp % 2 * 8) = o;
-                        }
-                    }
-                    lds_done();
-                    const int r = lane / 8, ch = lane % 8, row = wi * 128 + i * 16 + h * 8 + r, col = wj * 64 + ch * 8;
-                    struct __attribute__((aligned(16))) oct_t { out_t v[8]; } o = *reinterpret_cast<const oct_t *>(mine + r * 128 + (ch ^ r) * 16);
-                    if (row < t.rows && col < cols) {
-                        char *dst = c + ((long)(t.row + row) * g.cols + t.col + col) * OS;
-                        if (col + 8 <= cols) {
-                            stream_out(dst, o);
-                        } else {
-#pragma unroll
-                            for (int v = 0; v < 8; ++v)
-                                if (col + v < cols) reinterpret_cast<out_t *>(dst)[v] = o.v[v];
-                        }
-                    }
-                    lds_done();
-                }
         }
+#endif
     };
 
     // What has to have landed at the end of a phase, and how many younger loads may still be in flight (those of scales and stores, not

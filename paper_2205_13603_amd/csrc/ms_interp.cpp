@@ -756,7 +756,6 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
         if (code != 256256 && alone && ragged_aligned(op)) t.wi = t.wj = t.groups = 2;
         t.lds = (int64_t)t.groups * t.stages * (t.bm + t.bn) * 128 + (scaled ? 2 * (8 * t.bm * 4 + 256) : 0) + (table ? 4096 : 0);
         if (code == 256256 && op->d.in_dtype == MS_I8) t.lds += 3 * 2048; // scales of rows and columns of three tiles
-        if (code == 256256 && op->out_size == 2) t.lds += 8192; // where results are put together as lines
         if (code == 256256 && (table || op->d.kind == MS_OP_GROUPED_WGRAD)) t.lds += 2048; // experts without a whole tile; their order
     }
     return t;
