@@ -145,16 +145,17 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
         for (auto &x : extra) opts_joined += x + " ";
     }
     uint64_t k = mix64(key ^ source->hash ^ mix64(hash_bytes(opts_joined)) ^ mix64(0xC0DE000000000000ull ^ compiler_id()));
+    const std::string dir = cache_dir();
+    const uint64_t in_memory = k ^ hash_bytes(dir); // a kernel that is asked for lies in the directory that is set now, too
     {
         std::lock_guard<std::mutex> lk(g_mu);
-        auto it = g_codes.find(k);
+        auto it = g_codes.find(in_memory);
         if (it != g_codes.end()) {
             ++g_n_mem;
             *code_out = it->second.get();
             return MS_OK;
         }
     }
-    std::string dir = cache_dir();
     char fname[64];
     snprintf(fname, sizeof fname, "/%016" PRIx64 ".hsaco", k);
     std::unique_ptr<std::vector<char>> code(new std::vector<char>());
@@ -221,8 +222,8 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
         }
     }
     std::lock_guard<std::mutex> lk(g_mu);
-    auto it = g_codes.find(k);
-    if (it == g_codes.end()) it = g_codes.emplace(k, std::move(code)).first;
+    auto it = g_codes.find(in_memory);
+    if (it == g_codes.end()) it = g_codes.emplace(in_memory, std::move(code)).first;
     *code_out = it->second.get();
     return MS_OK;
 }
