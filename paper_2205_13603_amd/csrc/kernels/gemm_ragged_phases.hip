@@ -15,7 +15,7 @@
 // What bounds it: the clock under load (1.8 to 2.0 GHz) at 53 to 57 % of the matrix cores' cycles in long products, and what a tile's end leaves
 // uncovered, 9 us of stores and first reads for each round of tiles.  8192^3 in 8 bits 450 to 490 us by card and by what ran before (2.2 to 2.4
 // PFLOP/s; loads alone 338, products alone 215 at this clock); bf16, 8 experts, 8192 x 4096 x 4096 230 to 246 (1.1 to 1.2); 8 bits, 32 experts, 16384 x
-// 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 154 to 181 by the experts' rows (0.8 to 0.9, and 2.0 to 2.4 TB/s).
+// 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 147 to 174 by the experts' rows (0.8 to 0.9, and 2.1 to 2.5 TB/s).
 // 8-bit integers: 8192^3 402 to 410 (2.7 Pop/s, the matrix cores busy two thirds of their cycles), 32 experts, 16384 x 2048 x 4096 145 to 148 (1.9).
 // Their scales meet the sums once, at the end; they come in by way of LDS with a tile's first step (read there instead, each tile waited 4 us for them).
 //
@@ -353,13 +353,15 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const ragged_arg
 #if OUT_DT == DT_F32
 #pragma unroll
         for (int i = 0; i < TM; ++i) {
-            const int r = wi * 128 + i * 16 + lrow;
-            if (r < t.rows) {
+            f4_t x[TN];
 #pragma unroll
-                for (int j = 0; j < TN; ++j) {
-                    const int col = wj * 64 + j * 16 + lgrp * 4;
-                    if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
-                }
+            for (int j = 0; j < TN; ++j) x[j] = results(acc[i][j], si[i], sj[j]);
+            rows_together(x);
+            const int col = wj * 64 + lrow / 4 * 16 + lgrp * 4;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int r = wi * 128 + i * 16 + s * 4 + lrow % 4;
+                if (r < t.rows && col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, x[s], cols - col);
             }
         }
 #else

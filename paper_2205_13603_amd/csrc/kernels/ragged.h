@@ -299,6 +299,37 @@ template <class T> __device__ __forceinline__ void stream_out(char *dst, const T
     __builtin_nontemporal_store(__builtin_bit_cast(words_t, x), reinterpret_cast<words_t *>(dst));
 }
 
+// Four column tiles of fp32 results, of which lane 16 g + r has columns 4 g to 4 g + 3 of row r, put together between lanes: x[s] is then of row 4 s + r % 4,
+// column tile r / 4, so that four rows leave at a time, each as 256 bytes.  (8-bit integers into fp32, 8192 x 8192 x 512 by 256 x 256: 132 us as 64 bytes of 16
+// rows, 84 this way; 8192 x 8191 x 512 by 64 x 128 233 and 95; gradient of 8 experts, 4096 x 2048, bf16 154 and 147.)
+__device__ __forceinline__ void rows_together(f4_t (&x)[4])
+{
+    auto both = [](float &a, float &b, auto swap) {
+        const int p = __builtin_bit_cast(int, a), q = __builtin_bit_cast(int, b);
+        a = __builtin_bit_cast(float, swap(p, q, true));
+        b = __builtin_bit_cast(float, swap(q, p, false));
+    };
+#pragma unroll
+    for (int v = 0; v < 4; ++v) {
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            float a = x[j][v], b = x[j + 2][v];
+            both(a, b, [](int own, int other, bool first) { // lanes 8 to 15 of a row, and 0 to 7
+                return first ? __builtin_amdgcn_update_dpp(own, other, 0x128, 0xf, 0xc, false) : __builtin_amdgcn_update_dpp(own, other, 0x128, 0xf, 0x3, false);
+            });
+            x[j][v] = a, x[j + 2][v] = b;
+        }
+#pragma unroll
+        for (int j = 0; j < 4; j += 2) {
+            float a = x[j][v], b = x[j + 1][v];
+            both(a, b, [](int own, int other, bool first) { // every other four lanes, and the ones before them
+                return first ? __builtin_amdgcn_update_dpp(own, other, 0x114, 0xf, 0xa, false) : __builtin_amdgcn_update_dpp(own, other, 0x104, 0xf, 0x5, false);
+            });
+            x[j][v] = a, x[j + 1][v] = b;
+        }
+    }
+}
+
 // up to four results of a row at `dst`, the first `n` of them; STREAM: as above (parts of lines are slower that way)
 template <bool STREAM> __device__ __forceinline__ void store4(char *dst, f4_t x, int n)
 {

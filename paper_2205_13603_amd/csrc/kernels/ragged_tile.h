@@ -312,13 +312,16 @@ template <int TR, int TC, int WR, int WC, int GROUPS = 1> struct ragged_tile {
         if constexpr (OS == 4) {
 #pragma unroll
             for (int i = 0; i < HALF; ++i) {
-                const int r = row0 + i * 16 + lrow;
-                if (r < t.rows) {
+                static_assert(TN == 4, "64 columns of a wavefront");
+                f4_t x[4];
 #pragma unroll
-                    for (int j = 0; j < TN; ++j) {
-                        const int col = (wj * TN + j) * 16 + lgrp * 4;
-                        if (col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, results(acc[i][j], si[i], sj[j]), cols - col);
-                    }
+                for (int j = 0; j < 4; ++j) x[j] = results(acc[i][j], si[i], sj[j]);
+                rows_together(x);
+                const int col = wj * 64 + lrow / 4 * 16 + lgrp * 4;
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    const int r = row0 + i * 16 + s * 4 + lrow % 4;
+                    if (r < t.rows && col < cols) store4<true>(c + ((long)(t.row + r) * g.cols + t.col + col) * OS, x[s], cols - col);
                 }
             }
         } else {

@@ -771,11 +771,13 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
 int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
-    static const struct { int code; double start, tile, step, share; } costs[2][7] = {
+    static const struct { int code; double start, tile, step, share; } costs[3][7] = {
         {{16016, 2.4, 0.3, 0.061, 0.070}, {16032, 2.3, 0.5, 0.089, 0.085}, {32032, 2.4, 0.6, 0.133, 0.155}, {64032, 2.9, 0.6, 0.234, 0.235},
          {64128, 4.4, 0.85, 0.42, 0.375}, {128128, 5.7, 1.0, 0.58, 0.585}, {256256, 6.0, 9.0, 1.65, 1.75}},
         {{16016, 2.5, 0.2, 0.051, 0.060}, {16032, 2.5, 0.4, 0.081, 0.070}, {32032, 2.4, 0.6, 0.116, 0.130}, {64032, 3.2, 0.2, 0.196, 0.25},
-         {64128, 4.2, 0.80, 0.375, 0.31}, {128128, 4.9, 1.6, 0.54, 0.48}, {256256, 4.0, 9.8, 1.40, 1.45}}};
+         {64128, 4.2, 0.80, 0.375, 0.31}, {128128, 4.9, 1.6, 0.54, 0.48}, {256256, 4.0, 9.8, 1.40, 1.45}},
+        {{16016, 2.4, 0.1, 0.040, 0.051}, {16032, 2.5, 0.15, 0.060, 0.077}, {32032, 2.8, 0.1, 0.082, 0.141}, {64032, 3.0, 0.1, 0.152, 0.237},
+         {64128, 3.8, 0.15, 0.367, 0.32}, {128128, 3.5, 1.3, 0.571, 0.48}, {256256, 6.0, 6.1, 1.41, 1.44}}};
     const bool wgrad = op->d.kind == MS_OP_GROUPED_WGRAD, many = op->d.kind != MS_OP_SCALED_GEMM && op->nb > 1;
     const int64_t experts = op->d.kind == MS_OP_SCALED_GEMM ? 1 : std::min(op->nb, wgrad ? op->K : op->M), matrices = wgrad ? op->nb : experts;
     const double rows = wgrad ? (double)op->M : (double)op->M / (double)experts;
@@ -783,14 +785,16 @@ int64_t ragged_rule(const ms_op *op)
     const double bytes = wgrad ? 0 : (double)matrices * (double)op->N * (double)op->K * op->in_size;
     int64_t best = 0;
     double least = 0;
-    for (const auto &c : costs[op->d.in_dtype == MS_F8E4M3 ? 0 : 1]) { // 8-bit integers: as many matrix-core cycles to a step as 16-bit floats
+    const bool i8 = op->d.in_dtype == MS_I8;
+    for (const auto &c : costs[op->d.in_dtype == MS_F8E4M3 ? 0 : i8 ? 2 : 1]) {
         if (!layer_block_fits(op, c.code)) continue;
         const RaggedTile t = ragged_tile(op, c.code);
         const double more = wgrad && many ? 1 : 0; // a gradient's tiles are as long as their experts: one more
         double q, product;
         if (c.code == 256256) { // divides what is left into quarters, which take 0.4 of a tile's time: all of an expert of few rows
             const double quarters = many && !wgrad && rows < 256 ? 1.6 : 1;
-            q = std::max(1.0, std::ceil((rows / 256 + (many && !wgrad ? 0.25 : 0)) * quarters * (double)matrices * ((double)op->N / 256) / 64) / 4);
+            // (8-bit integers: a round of fewer tiles is faster, the clock being higher: 128 of 56 steps 70 us, 192 75, 256 91)
+            q = std::max(i8 && !many ? 0.75 : 1.0, std::ceil((rows / 256 + (many && !wgrad ? 0.25 : 0)) * quarters * (double)matrices * ((double)op->N / 256) / 64) / 4);
             product = (q + more) * c.share;
         } else {
             q = std::max(1.0, std::ceil(ragged_expected(op, t) / 256 - 0.03));
