@@ -767,7 +767,8 @@ RaggedTile ragged_tile(const ms_op *op, int64_t code)
 // (Fits of launches of 64 to 4096 whole tiles by 8 and 40 steps, operands in the L2s, contiguous along k; the others within 10 %.)
 // What it separates, measured on both sides: 8 bits, 256 x 2048 x 5440: 64 x 32 11.9 us, 64 x 128 21.8, 128 x 128 29.4; 1111 x 2056 x
 // 1360: 16.9, 14.5, 13.5 and 256 x 256 15.0; 32 experts, 16384 x 2048 x 4096: 128 x 128 212, 256 x 256 183.  bf16, one row for each of 16
-// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 260 drawn sizes of every kind it took 1.02 times the best block's time.
+// experts, 1024 x 2048: 16 x 16 9.7, 16 x 32 10.0, 64 x 128 16.5.  Over 260 drawn sizes of every kind it took 1.02 times the best block's time;
+// 8-bit integers over 160 1.04 times, 968 x 10784 x 10448 by 128 x 128 197, by 256 x 256 127.
 int64_t ragged_rule(const ms_op *op)
 {
     if (!ragged_aligned(op)) return 64128; // the one that reads element by element
