@@ -16,7 +16,7 @@
 // uncovered, 9 us of stores and first reads for each round of tiles.  8192^3 in 8 bits 450 to 490 us by card and by what ran before (2.2 to 2.4
 // PFLOP/s; loads alone 338, products alone 215 at this clock); bf16, 8 experts, 8192 x 4096 x 4096 230 to 246 (1.1 to 1.2); 8 bits, 32 experts, 16384 x
 // 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 147 to 174 by the experts' rows (0.8 to 0.9, and 2.1 to 2.5 TB/s).
-// 8-bit integers: 8192^3 402 to 410 (2.7 Pop/s, the matrix cores busy two thirds of their cycles), 32 experts, 16384 x 2048 x 4096 145 to 148 (1.9).
+// 8-bit integers: 8192^3 390 to 410 (2.7 to 2.8 Pop/s, the matrix cores busy 71 % of the cycles), 32 experts, 16384 x 2048 x 4096 139 to 148 (1.9).
 // Their scales meet the sums once, at the end; they come in by way of LDS with a tile's first step (read there instead, each tile waited 4 us for them).
 //
 // 8-bit floats: the products of a block of 128 k values are one instruction, whose four results per lane are added to the sums
