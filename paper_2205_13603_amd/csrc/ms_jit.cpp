@@ -14,11 +14,13 @@
 #include <map>
 #include <memory>
 #include <mutex>
+#include <set>
 
 namespace ms {
 
 static std::mutex g_mu;
 static std::map<uint64_t, std::unique_ptr<std::vector<char>>> g_codes;
+static std::set<std::pair<std::string, uint64_t>> g_kept; // directories, and the kernels in memory that have been read from or written into each
 struct Source {
     std::string text;
     uint64_t hash; // of the text: 150 KB a byte at a time took 0.2 ms of every build
@@ -122,6 +124,21 @@ static int32_t get_source(const std::string &name, const Source **src) // entrie
     return MS_OK;
 }
 
+// A kernel as a file, which other processes see whole or not at all.
+static void write_code(const std::string &dir, const std::string &name, const std::vector<char> &code)
+{
+    mkdir(dir.c_str(), 0777);
+    char tmpn[64];
+    snprintf(tmpn, sizeof tmpn, ".tmp.%d.%" PRIx64, (int)getpid(), (uint64_t)(uintptr_t)tmpn); // another thread's has another address
+    const std::string path = dir + name, tmp = path + tmpn;
+    FILE *f = fopen(tmp.c_str(), "wb");
+    if (!f) return;
+    bool ok = fwrite(code.data(), 1, code.size(), f) == code.size();
+    ok = fclose(f) == 0 && ok;
+    if (ok) rename(tmp.c_str(), path.c_str());
+    else unlink(tmp.c_str());
+}
+
 int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **code_out)
 {
     const Source *source = nullptr;
@@ -146,18 +163,23 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
     }
     uint64_t k = mix64(key ^ source->hash ^ mix64(hash_bytes(opts_joined)) ^ mix64(0xC0DE000000000000ull ^ compiler_id()));
     const std::string dir = cache_dir();
-    const uint64_t in_memory = k ^ hash_bytes(dir); // a kernel that is asked for lies in the directory that is set now, too
+    char fname[64];
+    snprintf(fname, sizeof fname, "/%016" PRIx64 ".hsaco", k);
     {
-        std::lock_guard<std::mutex> lk(g_mu);
-        auto it = g_codes.find(in_memory);
-        if (it != g_codes.end()) {
-            ++g_n_mem;
-            *code_out = it->second.get();
+        bool kept;
+        {
+            std::lock_guard<std::mutex> lk(g_mu);
+            auto it = g_codes.find(k);
+            *code_out = it == g_codes.end() ? nullptr : it->second.get();
+            if (*code_out) ++g_n_mem;
+            kept = dir.empty() || (*code_out && !g_kept.emplace(dir, k).second);
+        }
+        if (*code_out) { // in a directory that was set since it came here it lies from now on, too
+            struct stat st;
+            if (!kept && (stat((dir + fname).c_str(), &st) != 0 || (size_t)st.st_size != (*code_out)->size())) write_code(dir, fname, **code_out);
             return MS_OK;
         }
     }
-    char fname[64];
-    snprintf(fname, sizeof fname, "/%016" PRIx64 ".hsaco", k);
     std::unique_ptr<std::vector<char>> code(new std::vector<char>());
     if (!dir.empty()) {
         std::string blob;
@@ -207,23 +229,12 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
             std::lock_guard<std::mutex> lk(g_mu);
             ++g_n_compiled;
         }
-        if (!dir.empty()) {
-            mkdir(dir.c_str(), 0777);
-            char tmpn[96];
-            snprintf(tmpn, sizeof tmpn, "%s.tmp.%d.%" PRIx64, fname, (int)getpid(), (uint64_t)(uintptr_t)code.get());
-            std::string tmp = dir + tmpn;
-            FILE *f = fopen(tmp.c_str(), "wb");
-            if (f) {
-                bool ok = fwrite(code->data(), 1, code->size(), f) == code->size();
-                ok = fclose(f) == 0 && ok;
-                if (ok) rename(tmp.c_str(), (dir + fname).c_str());
-                else unlink(tmp.c_str());
-            }
-        }
+        if (!dir.empty()) write_code(dir, fname, *code);
     }
     std::lock_guard<std::mutex> lk(g_mu);
-    auto it = g_codes.find(in_memory);
-    if (it == g_codes.end()) it = g_codes.emplace(in_memory, std::move(code)).first;
+    auto it = g_codes.find(k);
+    if (it == g_codes.end()) it = g_codes.emplace(k, std::move(code)).first;
+    if (!dir.empty()) g_kept.emplace(dir, k);
     *code_out = it->second.get();
     return MS_OK;
 }
