@@ -619,7 +619,8 @@ int32_t ms_variant_launch_kernel(const ms_variant *v, int32_t instances, ms_vari
  * (invalid traces are skipped).  *n_built = kernels now in the cache. */
 int32_t ms_prebuild(const ms_op *op, const ms_space *space, const ms_trace *traces, int32_t n,
                     int32_t threads, int32_t *n_built);
-/* Directory of the on-disk kernel cache (NULL or "" = in-memory only).  What is asked for from here on is kept there, also where this process has compiled it before. */
+/* Directory of the on-disk kernel cache (NULL or "" = in-memory only).  What is asked for from here on is kept there; what
+ * a variant or a loaded kernel of this process holds is written there as it is, not compiled again. */
 int32_t ms_set_cache_dir(const char *path);
 /* Where this process got its kernels from so far (Section 4: building a candidate is part of the cost of measuring
  * it): kernels compiled now, code objects read from the on-disk cache, requests served from memory; and the

@@ -4,6 +4,7 @@
 
 #include <cstdarg>
 #include <cstdint>
+#include <memory>
 #include <string>
 #include <vector>
 
@@ -99,6 +100,7 @@ struct KernelSpec {
     std::vector<std::string> defines;
     std::string entry;         // kernel symbol
     std::string first;         // of a layer: the kernel that a launch runs ahead of it, if any
+    mutable std::shared_ptr<const std::vector<char>> held; // the code that jit_get_code found: in use as long as this is there
     unsigned block[3];
     unsigned grid[3];          // per instance; instances multiply grid[2]
     unsigned lds_dynamic;

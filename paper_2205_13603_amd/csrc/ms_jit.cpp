@@ -19,7 +19,7 @@
 namespace ms {
 
 static std::mutex g_mu;
-static std::map<uint64_t, std::unique_ptr<std::vector<char>>> g_codes;
+static std::map<uint64_t, std::shared_ptr<std::vector<char>>> g_codes; // entries stay until the process ends
 static std::set<std::pair<std::string, uint64_t>> g_kept; // directories, and the kernels in memory that have been read from or written into each
 struct Source {
     std::string text;
@@ -165,18 +165,28 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
     const std::string dir = cache_dir();
     char fname[64];
     snprintf(fname, sizeof fname, "/%016" PRIx64 ".hsaco", k);
+    // One that this directory is known to hold comes from memory, and so does one that a variant or a loaded module holds: it is written into a directory that
+    // was set since.  What nothing holds any more starts anew with a directory: a search there counts what it compiles as one in a fresh process does.
     {
-        bool kept;
+        std::shared_ptr<std::vector<char>> found;
+        bool kept = true;
         {
             std::lock_guard<std::mutex> lk(g_mu);
             auto it = g_codes.find(k);
-            *code_out = it == g_codes.end() ? nullptr : it->second.get();
-            if (*code_out) ++g_n_mem;
-            kept = dir.empty() || (*code_out && !g_kept.emplace(dir, k).second);
+            if (it != g_codes.end()) {
+                kept = dir.empty() || g_kept.count({dir, k});
+                if (kept || it->second.use_count() > 1) {
+                    found = it->second;
+                    ++g_n_mem;
+                    if (!kept) g_kept.emplace(dir, k);
+                }
+            }
         }
-        if (*code_out) { // in a directory that was set since it came here it lies from now on, too
+        if (found) {
             struct stat st;
-            if (!kept && (stat((dir + fname).c_str(), &st) != 0 || (size_t)st.st_size != (*code_out)->size())) write_code(dir, fname, **code_out);
+            if (!kept && (stat((dir + fname).c_str(), &st) != 0 || (size_t)st.st_size != found->size())) write_code(dir, fname, *found);
+            *code_out = found.get();
+            spec.held = found;
             return MS_OK;
         }
     }
@@ -232,10 +242,11 @@ int32_t jit_get_code(const KernelSpec &spec, uint64_t key, std::vector<char> **c
         if (!dir.empty()) write_code(dir, fname, *code);
     }
     std::lock_guard<std::mutex> lk(g_mu);
-    auto it = g_codes.find(k);
-    if (it == g_codes.end()) it = g_codes.emplace(k, std::move(code)).first;
+    std::shared_ptr<std::vector<char>> &own = g_codes[k];
+    if (!own) own = std::move(code);
     if (!dir.empty()) g_kept.emplace(dir, k);
-    *code_out = it->second.get();
+    *code_out = own.get();
+    spec.held = own;
     return MS_OK;
 }
 

@@ -286,6 +286,7 @@ struct LoadedKernel {
     hipModule_t mod;
     hipFunction_t fn, first; // first: runs ahead of fn, null if there is none
     int device, compute_units;
+    std::shared_ptr<const std::vector<char>> held;
 };
 static std::mutex g_layers_mu;
 static std::map<std::pair<const std::vector<char> *, int>, LoadedKernel> g_layers;
@@ -314,7 +315,7 @@ static int32_t load_layer(ms_variant *v, int dev, const LoadedKernel **loaded)
     {
         std::lock_guard<std::mutex> lk(g_layers_mu);
         if (g_layers.find({v->code, dev}) == g_layers.end()) { // no other thread was quicker
-            LoadedKernel k = {nullptr, nullptr, nullptr, dev, prop.multiProcessorCount};
+            LoadedKernel k = {nullptr, nullptr, nullptr, dev, prop.multiProcessorCount, v->spec.held};
             HIP_TRY(hipModuleLoadData(&k.mod, v->code->data()));
             hipError_t e = hipModuleGetFunction(&k.fn, k.mod, v->spec.entry.c_str());
             if (e == hipSuccess && !v->spec.first.empty()) e = hipModuleGetFunction(&k.first, k.mod, v->spec.first.c_str());

@@ -21,13 +21,14 @@ def test_a_kernel_lies_in_the_directory_that_is_set(tmp_path):
         B.set_cache_dir(os.environ.get("MS_CACHE_DIR") or os.path.join(ROOT, "paper_2205_13603_amd", "kcache"))
 
 
-def test_a_kernel_in_memory_is_not_built_again_for_another_directory(tmp_path):
-    """What the process holds goes into the new directory as it is, into one without a place for it not at all; what lies there already stays."""
+def test_a_kernel_in_use_is_not_built_again_for_another_directory(tmp_path):
+    """What a variant holds goes into the new directory as it is, into one without a place for it not at all; what lies there already stays."""
     op = B.expert_order_op(64, 3, 2)
+    held = []
 
     def build():
         before = B.jit_stats()
-        B.Variant(op, op.space(), B.default_trace(op.space()))
+        held.append(B.Variant(op, op.space(), B.default_trace(op.space())))
         after = B.jit_stats()
         return [after[k] - before[k] for k in ("compiled", "from_disk", "from_memory")]
 
