@@ -4,7 +4,8 @@
 //   softmax, over the sum   dx_{id_j} = q_j (g_j - sum_i g_i q_i)
 //   sigmoid                 dx_{id_j} = g_j s_j (1 - s_j)
 //   sigmoid, over the sum   dx_{id_j} = (g_j - sum_i g_i q_i) q_j (1 - s_j)
-// and zero elsewhere.  Ids outside of the experts are no choices.  A choice that occurs twice adds up, in the order of the choices.
+// and zero elsewhere.  Ids outside of the experts are no choices.  A choice that occurs twice adds up, in the order of the choices.  Over the sum, p and s are taken
+// relative to the largest chosen one's exponential: s e^-h = e^(min(x, 0) - h) / (1 + e^-|x|), h the largest min(x, 0).
 //
 // LANES lanes take a token, VALUES experts each: the chosen ones' parts go into the token's row in LDS, from where all lanes take theirs.
 //
@@ -74,6 +75,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const route_grad
     if constexpr (!SIGMOID) {
         high = max_lanes(high);
         high = high > -__builtin_inff() ? high : 0.f; // a row without experts
+    } else if constexpr (RENORM) {
+        high = __builtin_fminf(max_lanes(high), 0.f);
+        high = high > -__builtin_inff() ? high : 0.f;
     }
     if constexpr (DENSE) {
         float sum = 0;
@@ -92,7 +96,9 @@ extern "C" __global__ void __launch_bounds__(THREADS) ms_kernel(const route_grad
         for (int r = 0; r < ROUNDS; ++r) {
             if constexpr (SIGMOID) {
                 const float t = expf(-__builtin_fabsf(logit[r])), a = 1 / (1 + t), b = t / (1 + t); // of |x| and -|x|
-                s[r] = logit[r] < 0 ? b : a;
+                // over their sum: times e^-high, so that the largest is one half at least, however small the scores are (fp32 has bits of them down to logits of -103 only)
+                if constexpr (RENORM) s[r] = expf(__builtin_fminf(logit[r], 0.f) - high) * a;
+                else s[r] = logit[r] < 0 ? b : a;
                 slope[r] = logit[r] < 0 ? a : b; // 1 - s
             } else {
                 s[r] = expf(logit[r] - high);

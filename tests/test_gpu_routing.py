@@ -322,6 +322,73 @@ def test_gradient_is_that_of_the_weights(scores, renormalise):
     assert bool(((dx.double() * u.double()).sum(1) - slope).abs().le(dw.double().abs().sum(1) * (h * h / 6 * 32 + 45 * 2.0 ** -24 / h)).all())
 
 
+LEVELS = (300.0, 90.0, 0.0, -60.0, -87.0, -90.0, -95.0, -100.0, -103.0, -110.0, -300.0, -600.0)
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("E,K", [(8, 3), (100, 20)])
+def test_gradient_of_small_scores_over_their_sum(E, K, kind):
+    """Sigmoids that fp32 holds as few bits or none: their parts of the sum are ordinary numbers.  In 64 bits by logarithms, weights = softmax(log sigmoid).
+    Tolerances as above: a difference of two logits is off by 2^-24 of itself, d, and so its exponential by less than d e^-d, half a step of the largest."""
+    T = 4 * len(LEVELS)
+    op = B.route_grad_op(T, E, K, kind, scores="sigmoid", renormalise=True, scale=2.5)
+    g = rng(K)
+    level = torch.tensor(LEVELS).repeat_interleave(4)[:, None]
+    x = normal(g, T, E) + level
+    ids = torch.stack([torch.randperm(E, generator=g)[:K] for _ in range(T)]).int()
+    for t in range(1, T, 4):  # one ordinary logit among them
+        x[t, int(ids[t, 1])] = 0.5
+    for t in range(2, T, 4):  # a choice that is none
+        ids[t, 0] = -1
+    for t in range(3, T, 4):  # the same for all
+        x[t] = level[t]
+    x = x.to(TYPES[kind])
+    dw = normal(g, T, K)
+    real = ids >= 0
+    of = x.double().requires_grad_(True)
+    logs = torch.nn.functional.logsigmoid(of).gather(1, torch.where(real, ids, 0).long())
+    w = torch.softmax(torch.where(real, logs, torch.full_like(logs, -INF)), 1)
+    (w * dw.double() * 2.5).sum().backward()
+    parts, q = (dw.double() * 2.5).abs() * real, w.detach()
+    mag = torch.zeros(T, E, dtype=torch.float64).scatter_add_(1, torch.where(real, ids, 0).long(), parts * q + (parts * q).sum(1, keepdim=True) * q)
+    assert bool((of.grad.abs().amax(1)[level[:, 0] < 0] > 1e-4).sum() > T // 3)  # no level's gradients vanish
+    space = op.space()
+    for c in range(space.slots[0].n_candidates):
+        if not space.slots[0].weight[c]:
+            continue
+        v = variant(op, space.slots[0].candidates[c])
+        if v is None:
+            continue
+        (dx,) = call(v, [dev(x), dev(ids), dev(dw)], [((T, E), TYPES[kind])])
+        tol = of.grad.abs() * HALF_STEP[kind] * 1.01 + mag * 64 * 2.0 ** -24 + (2.0 ** -25 if kind == "f16" else 1e-37)
+        off = ((dx.double() - of.grad).abs() <= tol).all(1)
+        assert bool(off.all()), "at logits about %s" % sorted(set(level[~off, 0].tolist()))
+
+
+@pytest.mark.parametrize("level", [-95.0, -110.0, -600.0])
+def test_gradient_of_small_scores_is_that_of_their_weights(level):
+    """As test_gradient_is_that_of_the_weights, where fp32 holds no sigmoid: steps of 2^-8 and logits 1/8 apart are exact down to -1024 (2^-13)."""
+    T, E, K, h = 60, 24, 5, 2.0 ** -8
+    kw = dict(scores="sigmoid", renormalise=True)
+    f, v = variant(B.route_op(T, E, K, **kw)), variant(B.route_grad_op(T, E, K, **kw))
+    if f is None:
+        return
+    g = rng(12)
+    x = torch.stack([torch.randperm(E, generator=g) for _ in range(T)]).float() / 8 + level
+    u = torch.randint(0, 2, (T, E), generator=g).float() * 2 - 1
+    dw = normal(g, T, K)
+    shapes = [((T, K), torch.int32), ((T, K), torch.float32)]
+    ids, _ = call(f, [dev(x), None], shapes)
+    (dx,) = call(v, [dev(x), dev(ids), dev(dw)], [((T, E), torch.float32)])
+    sides = []
+    for step in (h, -h):
+        i, w = call(f, [dev(x + step * u), None], shapes)
+        assert torch.equal(i, ids)
+        sides.append((w.double() * dw.double()).sum(1))
+    slope = (sides[0] - sides[1]) / (2 * h)
+    assert bool(((dx.double() * u.double()).sum(1) - slope).abs().le(dw.double().abs().sum(1) * (h * h / 6 * 32 + 45 * 2.0 ** -24 / h)).all())
+
+
 def test_gradient_over_its_logits():
     T, E, K = 90, 40, 4
     v = variant(B.route_grad_op(T, E, K, "bf16"))
