@@ -115,7 +115,7 @@ def precompile_all(threads=4):
 def layer_ops():
     """One operator for each set of kernels of the layers (their kernels do not depend on sizes): types, layouts, whole 16 bytes or not.  The choice of
     experts and its gradient are not among them (their kernels go by the powers of two of experts and choices, and a router's few are built at its
-    first use), rows of experts only in bf16."""
+    first use), rows of experts only from bf16 (those from fp16, fp32 and 8 bits likewise)."""
     halves = ("f16", "bf16")
     ops = [B.rms_norm_op(64, 512, t, out, residual) for t in halves + ("f32",) for out in (t, "f8") for residual in (False, True)]
     for rows, cols, depth in ((64, 512, 256), (64, 509, 250), (1024, 8448, 256)):  # the last: more workgroups than compute units
@@ -128,12 +128,12 @@ def layer_ops():
                 ops.append(B.grouped_wgrad_op(2, rows, cols, depth, t, out))
     ops += [B.spread_rows_op(8, 2, 512, 16, "bf16", out) for out in ("bf16", "i8", "f8")] + [B.join_grad_op(8, 2, 512, 16)]
     ops += [B.join_rows_op(8, 2, 512, 16, "bf16", out, residual=residual) for out in ("bf16", "f32") for residual in (False, True)]
-    ops += [B.expert_order_op(experts, tokens, 1) for experts in (64, 256, 1024) for tokens in (64, 1024, 1 << 16)]
+    ops += [B.expert_order_op(experts, tokens, 1) for experts in (64, 256, 1024) for tokens in (64, 256, 1024, 1 << 16)]
     return ops
 
 
 def precompile_layers(threads=4):
-    """Every kernel that a rule of theirs can choose, so that no size of theirs compiles at its first call."""
+    """Every kernel that a rule of layer_ops() can choose: no size of these operators and types compiles at its first call."""
     n = 0
     for op in layer_ops():
         space = op.space()

@@ -430,6 +430,20 @@ def test_expert_order(E, T, K, code):
         assert torch.equal(offsets, want) and torch.equal(place, places), k
 
 
+@pytest.mark.parametrize("E", [1, 64, 256, 1024])
+@pytest.mark.parametrize("T,K", [(65, 1), (20, 8), (32, 8), (257, 1)])
+def test_order_of_a_few_wavefronts(T, K, E):
+    """A decoding batch: workgroups of one, four and sixteen wavefronts, and the counts at which they change."""
+    v = variant(B.expert_order_op(E, T, K))
+    if v is None:
+        return
+    g = rng(T + E)
+    for ids in (torch.randint(0, E, (T, K), generator=g).int(), torch.randint(-2, E + 2, (T, K), generator=g).int(), torch.full((T, K), E - 1).int()):
+        offsets, place = call(v, [dev(ids)], [((E + 1,), torch.int32), ((T, K), torch.int32)])
+        want, places = order_definition(ids, E)
+        assert torch.equal(offsets, want) and torch.equal(place, places)
+
+
 def test_order_of_several_instances():
     for E, T, K in ((7, 9, 2), (70, 3000, 4)):
         R = 3

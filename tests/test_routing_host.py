@@ -5,7 +5,7 @@ import subprocess
 import numpy as np
 import pytest
 
-from paper_2205_13603_amd import binding as B, devmem
+from paper_2205_13603_amd import binding as B, devmem, tuned
 
 OPS = {
     "route": lambda: B.route_op(37, 60, 6, "bf16"),
@@ -237,6 +237,30 @@ def test_rules():
     assert block(B.route_op(100000, 1024, 8)) == 32 and block(B.route_op(100000, 300, 8)) == 16 and block(B.route_op(16384, 60, 6)) == 8
     assert [block(B.join_rows_op(9, 8, N, 72)) for N in (8, 512, 513, 2050, 8192, 8193, 20000)] == [1, 1, 2, 5, 16, 10, 14]
     assert [block(B.expert_order_op(8, T, 8)) for T in (1, 500, 16384, 1 << 20)] == [1, 4, 1, 16] and [block(B.expert_order_op(E, 16384, 8)) for E in (64, 256, 1024)] == [1, 1, 2]
+
+
+def test_no_size_needs_a_kernel_that_is_not_built_ahead():
+    """Of the operators and types that are built ahead: the kernels of drawn sizes are among those of layer_ops(), for every block of theirs."""
+    import random
+    built = set()
+    for op in tuned.layer_ops():
+        space = op.space()
+        for c in range(space.slots[0].n_candidates):
+            if space.slots[0].weight[c]:
+                built.add(B.trace_validate(op, space, B.make_trace(space, [[space.slots[0].candidates[c]]])).key)
+    r = random.Random(7)
+    some = lambda least, most: round(least * (most / least) ** r.random())
+    ops = [B.expert_order_op(E, T, K) for E in (64, 256, 1024) for T, K in ((1, 64), (13, 5), (20, 8), (12, 6), (40, 2), (32, 8), (257, 1), (4097, 1), (1 << 23, 8))]
+    ops += [B.expert_order_op(some(1, 1024), some(1, 1 << 20), some(1, 16)) for _ in range(60)]
+    for _ in range(40):
+        T, K, N = some(1, 20000), some(1, 16), some(1, 20000)
+        ops += [B.spread_rows_op(T, K, N, T * K, "bf16", r.choice(("bf16", "i8", "f8"))), B.join_grad_op(T, K, N, T * K),
+                B.join_rows_op(T, K, N, T * K, "bf16", r.choice(("bf16", "f32")), residual=r.random() < 0.5)]
+        ops += [B.scaled_gemm_op(T, N, some(1, 20000), r.choice(("bf16", "f16", "f32")), in_dtype=r.choice(("f8", "i8"))),
+                B.grouped_gemm_op(some(1, 64), T, N, some(1, 20000), True, r.choice(("f8", "i8")), r.choice(("bf16", "f16", "f32")))]
+    for op in ops:
+        p = B.trace_validate(op, op.space(), B.default_trace(op.space()))
+        assert p.key in built, (op.work(), p.body, p.body_tile, p.threads)
 
 
 def test_sampled_composed_and_searched():
