@@ -683,7 +683,7 @@ void resolve_body(const ms_op *op, ms_variant_params *p)
 // ---- layers of language models: kernels that take sizes as arguments, chosen by what a workgroup works on
 
 // B (the products) contiguous along k
-bool ragged_by_k(const ms_op *op) { return op->d.kind != MS_OP_GROUPED_WGRAD && op->d.b_strides[1] == 1 && op->d.b_strides[2] >= op->K; }
+bool ragged_by_k(const ms_op *op) { return op->d.kind != MS_OP_GROUPED_WGRAD && !is_routing(op->d.kind) && op->d.b_strides[1] == 1 && op->d.b_strides[2] >= op->K; }
 
 // loads of 16 bytes: rows and extents of whole 16 bytes
 bool ragged_aligned(const ms_op *op)

@@ -258,6 +258,7 @@ def test_no_size_needs_a_kernel_that_is_not_built_ahead():
                 B.join_rows_op(T, K, N, T * K, "bf16", r.choice(("bf16", "f32")), residual=r.random() < 0.5)]
         ops += [B.scaled_gemm_op(T, N, some(1, 20000), r.choice(("bf16", "f16", "f32")), in_dtype=r.choice(("f8", "i8"))),
                 B.grouped_gemm_op(some(1, 64), T, N, some(1, 20000), True, r.choice(("f8", "i8")), r.choice(("bf16", "f16", "f32")))]
+    ops.append(B.join_grad_op(50, 1, 1, 50))  # its strides could be those of either order
     for op in ops:
         p = B.trace_validate(op, op.space(), B.default_trace(op.space()))
         assert p.key in built, (op.work(), p.body, p.body_tile, p.threads)
