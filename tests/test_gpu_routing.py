@@ -444,6 +444,27 @@ def test_order_of_a_few_wavefronts(T, K, E):
         assert torch.equal(offsets, want) and torch.equal(place, places)
 
 
+@pytest.mark.parametrize("E,T,K", [(1024, 1050001, 8), (256, 1 << 22, 3), (7, 1 << 21, 32)])
+def test_order_of_millions_of_choices(E, T, K):
+    """Up to the most that there may be, MS_MAX_CHOICES; the definition by a stable sort on the GPU."""
+    v = variant(B.expert_order_op(E, T, K))
+    if v is None:
+        return
+    n = T * K
+    ids = torch.randint(0, E, (n,), generator=rng(E)).int().cuda()
+    ids[::1001] = -1
+    offsets, place = torch.full((E + 1,), 7, dtype=torch.int32, device="cuda"), torch.full((n,), 7, dtype=torch.int32, device="cuda")
+    ws = torch.full((v.workspace_bytes(),), 0x55, dtype=torch.uint8, device="cuda")
+    v.launch([ids.data_ptr()], [offsets.data_ptr(), place.data_ptr()], stream=devmem.current_stream(), workspace=ws.data_ptr())
+    key = torch.where(ids < 0, torch.full_like(ids, E), ids).short()
+    order = key.sort(stable=True)[1]
+    counts = torch.bincount(key.int(), minlength=E + 1)[:E]
+    real = int(counts.sum())
+    want = torch.full((n,), -1, dtype=torch.int32, device="cuda")
+    want[order[:real]] = torch.arange(real, dtype=torch.int32, device="cuda")
+    assert torch.equal(place, want) and int(offsets[0]) == 0 and torch.equal(offsets[1:].long(), counts.cumsum(0))
+
+
 def test_order_of_several_instances():
     for E, T, K in ((7, 9, 2), (70, 3000, 4)):
         R = 3
