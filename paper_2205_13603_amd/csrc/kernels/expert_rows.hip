@@ -10,7 +10,8 @@
 // lies beyond again.  A token's places and weights lie in the lanes of each of its wavefronts, from where scalar registers take them: a row's
 // address is computed once, by the scalar unit.
 //
-// What bounds it is memory: bf16, 4096 x 2048 to 8 choices into 8-bit integers 14.8 us (5.7 TB/s), as they are 26.2 (5.8); back 28.4 (5.3, rows of 4 KiB read in any
+// What bounds it is memory: bf16, 4096 x 2048 to 8 choices into 8-bit integers 14.8 us (5.7 TB/s), into 8-bit floats 15.3 (5.6; from fp32 17.5, 5.9), as they are 26.2 (5.8),
+// 8 bits as they are 14.4 (integers) and 15.1 (floats); back 28.4 (5.3, rows of 4 KiB read in any
 // order); gradients 57 (5.0, as much written as read; 3000 x 2050 to 6 choices, whose rows are no whole 16 bytes, 30 to 36 by what the card's last level cache
 // holds).  Results stay out of the L2s: kept there 4096 x 2048 to 8 choices takes 32 us instead of 26, back 32 instead of 28.  Few tokens: the launch.
 #include "common.h"

@@ -12,11 +12,11 @@
 // Whole tiles of a last round that would leave most workgroups without one, and the rests of experts' rows of up to 128, are made in
 // quarters at the end, by all eight wavefronts of a workgroup each.
 //
-// What bounds it: the clock under load (1.8 to 2.0 GHz) at 53 to 57 % of the matrix cores' cycles in long products, and what a tile's end leaves
+// What bounds it: the clock under load (1.8 to 2.0 GHz) at 53 to 57 % of the matrix cores' cycles in long products of 8- and 16-bit floats, and what a tile's end leaves
 // uncovered, 9 us of stores and first reads for each round of tiles.  8192^3 in 8 bits 450 to 490 us by card and by what ran before (2.2 to 2.4
 // PFLOP/s; loads alone 338, products alone 215 at this clock); bf16, 8 experts, 8192 x 4096 x 4096 230 to 246 (1.1 to 1.2); 8 bits, 32 experts, 16384 x
 // 2048 x 4096 168 to 179 (1.6); gradient of 8 experts, 4096 x 2048 into fp32 147 to 174 by the experts' rows (0.8 to 0.9, and 2.1 to 2.5 TB/s).
-// 8-bit integers: 8192^3 390 to 410 (2.7 to 2.8 Pop/s, the matrix cores busy 71 % of the cycles), 32 experts, 16384 x 2048 x 4096 139 to 148 (1.9).
+// 8-bit integers: 8192^3 380 to 430 by card (2.6 to 2.9 Pop/s, the matrix cores busy 71 % of the cycles), 32 experts, 16384 x 2048 x 4096 139 to 157 (1.8 to 2.0).
 // Their scales meet the sums once, at the end; they come in by way of LDS with a tile's first step (read there instead, each tile waited 4 us for them).
 //
 // 8-bit floats: the products of a block of 128 k values are one instruction, whose four results per lane are added to the sums

@@ -6,7 +6,8 @@
 //
 // More choices than one workgroup takes: a first kernel counts each run's experts (counts), and each workgroup adds up what lies ahead of its own.
 //
-// What bounds it is latency: 16 choices 4.5 us, the launch; 131072 choices of 256 experts 7.2, of which the second launch is 2; 524288 10.0.
+// What bounds it is latency: 16 choices 4.5 us, the launch; 131072 choices of 256 experts 7.2, of which the second launch is 2; 524288 10.3, 2^20 12.4, 2^23 56.
+// Beyond that it is the counts, of which each run reads those of all: 2^26 choices 1143 us for 0.5 GB of choices and places, 1024 experts 3458.
 #include "common.h"
 
 struct order_args {

@@ -12,7 +12,7 @@
 // larger of one block's ascending and the other's descending list), then the lanes' lists meet in log2(LANES) steps the same way, after which all
 // lanes have the token's.  Groups of a power of two experts find their best in the lanes that hold them, others by way of LDS.
 //
-// What bounds it are the vector ALUs: 16384 x 256 in fp32, sigmoid, bias, 8 groups, 12.3 us, of which each SIMD issues 4700 instructions for 7.8 us
+// What bounds it are the vector ALUs: 16384 x 256 in fp32, sigmoid, bias, 8 groups, 12.3 us, of which each SIMD issues 5270 instructions for some 9 us
 // (a third forms scores, a third sorts, a sixth finds groups); the logits take 2.7 from memory.  Choices by logits alone, 16384 x 128: 4.4 us, the launch.
 // Wavefronts that go on to further tokens with the next logits under way take 13.2: what is hoisted out of their loop costs half the wavefronts.
 // One token 4.5 us, the launch.
@@ -103,7 +103,7 @@ __device__ __forceinline__ double without_index(double k) { return of_halves(hig
 // k, or something like NONE
 __device__ __forceinline__ double only_if(bool there, double k) { return of_halves(there ? high_of(k) : high_of(NONE), low_of(k)); }
 
-// e^x, |x| <= 710, within 2^-45 of it: 2^n times a polynomial of degree 9 in the rest r, |r| <= ln(2) / 2, that meets e^r in the ten Chebyshev points of a
+// e^x, |x| <= 710, within 2^-44.4 of it (up to 100, where ln(2) as one number costs nothing yet, 2^-45.3): 2^n times a polynomial of degree 9 in the rest r, |r| <= ln(2) / 2, that meets e^r in the ten Chebyshev points of a
 // little more than that (2^-45.6).  The coefficients lie in scalar registers: as literals each would cost two moves.
 struct series_t { double c[10], per_ln2, ln2, round; };
 __device__ __forceinline__ series_t series()
